@@ -13,7 +13,8 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libconvfwd.so")
 INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 
-SOURCES = ("conv_kernels.hip", "split_kernels.hip", "conv_api.cpp", "select.cpp", "split_route.cpp", "workspace.cpp")
+SOURCES = ("conv_kernels.hip", "split_kernels.hip", "seq_scan.hip", "seq_norm.hip", "seq_conv.hip",
+           "conv_api.cpp", "select.cpp", "split_route.cpp", "workspace.cpp", "seq_api.cpp")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

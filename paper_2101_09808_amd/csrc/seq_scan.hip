@@ -1,0 +1,808 @@
+// The selective scan: forward, backward, one token.
+//
+//   h[s](t) = a[s](t) h[s](t-1) + x(t) B[s](t),  a = exp(dt A[s]),  x = dt u
+//   y(t) = sum_s C[s](t) h[s](t) + Dskip u(t),   out = y z sigmoid(z)
+//
+// A step of a state is an exponential (four times the price of a product) and
+// about five multiply-adds, S of them for every element read: bound by the
+// vector ALU.  The recurrence is composed along the length: a row of sixteen
+// lanes takes a chunk of 128 steps of one channel, eight steps a lane.  Each
+// lane folds its steps (state from zero, and the decay over them), the pairs
+// (decay, state) are scanned over the row by DPP in four levels, and each lane
+// runs its eight steps again from the state that reaches it.  So a step's
+// exponential and products are formed once, the scan costs an eighth of its
+// sixteen instructions a step, and nothing but dt, x and y of eight steps is
+// held over the states.  A wave is four channels, a workgroup 4 NW of one
+// group: they share B and C, staged in LDS as fp32, the next chunk's under way
+// meanwhile.  Workgroups walk along the length.  Where rows are too few to fill
+// the chip the length is cut into segments: a first kernel finds what each
+// segment alone makes of a zero state, the second composes those before its
+// own.
+#include <type_traits>
+
+#include "seq_device.h"
+#include "seq_internal.h"
+
+namespace seqops {
+namespace {
+
+constexpr int kChunk = SEQ_SCAN_CHUNK;  // 16 lanes of 8 steps
+constexpr int kBatch = 2;               // states between two exchanges of dB and dC
+
+template <typename T>
+struct ScanArgs {
+  int N, D, L, S, G, per;  // per: channels of a group
+  int softplus;
+  int blks, segs, seg_chunks, chunks;
+  int64_t u_n, u_d, delta_n, delta_d, z_n, z_d, dout_n, dout_d, B_n, B_g, B_s, C_n, C_g, C_s;
+  const T *u, *delta, *z, *B, *C;
+  const float *A, *Dskip, *bias, *initial;
+  const int32_t* lengths;
+  T* out;
+  float *final_state, *checkpoints;
+  const T* dout;
+  const float* dfinal;
+  T *du, *ddelta, *dz, *dB, *dC;
+  float *dA, *dD, *dbias, *dinitial;
+  // scratch
+  float *ends, *end_dt;    // [N][segs][D][S], [N][segs][D]
+  float* part_bc;          // [N][G][blks][S][2][chunks * 128], a chunk's steps as in LDS
+  float *part_A, *part_D;  // [N][segs][D][S], [N][segs][D][2] (Dskip, delta_bias)
+};
+
+// Where a thread stands: wave of four channels, a row of sixteen lanes each.
+struct Place {
+  int lane, wave, row, tl;
+  int n, g, blk, seg;
+  int d0;    // the wave's first channel
+  int left;  // how many of its four there are (none: 0 or less)
+  int d;     // the row's channel; one that exists, if its own does not
+  bool ok;
+};
+template <typename T>
+__device__ __forceinline__ Place place(const ScanArgs<T>& a) {
+  Place p;
+  p.lane = threadIdx.x & 63;
+  p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  p.row = p.lane >> 4, p.tl = p.lane & 15;
+  uint32_t b = blockIdx.x;
+  p.blk = int(b % a.blks), b /= a.blks;
+  p.g = int(b % a.G), b /= a.G;
+  p.seg = int(b % a.segs), p.n = int(b / a.segs);
+  const int cw = (p.blk * int(blockDim.x >> 6) + p.wave) * 4;
+  p.left = a.per - cw;
+  p.d0 = p.g * a.per + cw;
+  p.ok = p.row < p.left;
+  p.d = p.ok ? p.d0 + p.row : p.g * a.per + a.per - 1;
+  return p;
+}
+
+// A chunk of B (and C) in LDS: a state's steps in two runs of 64, the first and
+// the last four steps of every lane, so that a lane's reads are whole 16-byte
+// banks next to its neighbours'.
+template <typename T, int NB>
+struct Stage {
+  Raw8<T> raw[NB];
+  // rows 0..S-1 are first's states, the others second's
+  __device__ __forceinline__ void load(const T* first, int64_t first_s, const T* second, int64_t second_s, int S,
+                                       int rows, int t0, int len) {
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      const int i = threadIdx.x + k * blockDim.x, r = i >> 4, t = t0 + (i & 15) * 8;
+      if (r < rows) raw[k] = load8((r < S ? first + r * first_s : second + (r - S) * second_s) + t, len - t);
+    }
+  }
+  __device__ __forceinline__ void store(float* lds, int rows) const {
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      const int i = threadIdx.x + k * blockDim.x, r = i >> 4;
+      if (r < rows) {
+        float v[8];
+        unpack8(raw[k], v);
+        float* at = lds + r * kChunk + (i & 15) * 4;
+        *reinterpret_cast<f32x4*>(at) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4*>(at + 64) = f32x4{v[4], v[5], v[6], v[7]};
+      }
+    }
+  }
+};
+__device__ __forceinline__ void lds8(const float* lds, int tl, float* v) {
+  const f32x4 lo = *reinterpret_cast<const f32x4*>(lds + tl * 4), hi = *reinterpret_cast<const f32x4*>(lds + 64 + tl * 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
+}
+
+// The states that reach each lane of a row: H (the lane's steps from zero) and
+// P (their decay) become the state behind the lane; the state before it is
+// returned.  `in` reaches lane 0.
+__device__ __forceinline__ float scan_row(float H, float P, float in, int tl) {
+  H = __builtin_fmaf(P, tl == 0 ? in : 0.f, H);
+  H = __builtin_fmaf(P, dpp0<kRowShr + 1>(H), H), P *= dpp0<kRowShr + 1>(P);
+  H = __builtin_fmaf(P, dpp0<kRowShr + 2>(H), H), P *= dpp0<kRowShr + 2>(P);
+  H = __builtin_fmaf(P, dpp0<kRowShr + 4>(H), H), P *= dpp0<kRowShr + 4>(P);
+  H = __builtin_fmaf(P, dpp0<kRowShr + 8>(H), H);
+  return dpp<kRowShr + 1>(in, H);
+}
+// The same from right to left; `in` reaches lane 15.
+__device__ __forceinline__ float scan_row_back(float H, float P, float in, int tl) {
+  H = __builtin_fmaf(P, tl == 15 ? in : 0.f, H);
+  H = __builtin_fmaf(P, dpp0<kRowShl + 1>(H), H), P *= dpp0<kRowShl + 1>(P);
+  H = __builtin_fmaf(P, dpp0<kRowShl + 2>(H), H), P *= dpp0<kRowShl + 2>(P);
+  H = __builtin_fmaf(P, dpp0<kRowShl + 4>(H), H), P *= dpp0<kRowShl + 4>(P);
+  H = __builtin_fmaf(P, dpp0<kRowShl + 8>(H), H);
+  return dpp<kRowShl + 1>(in, H);
+}
+// A row's sum in its lane 15.
+__device__ __forceinline__ float row_sum(float v) {
+  v += dpp0<kRowShr + 1>(v);
+  v += dpp0<kRowShr + 2>(v);
+  v += dpp0<kRowShr + 4>(v);
+  v += dpp0<kRowShr + 8>(v);
+  return v;
+}
+
+// dt of eight steps (zero behind the end: the state stands still) and its sum.
+template <typename T>
+__device__ __forceinline__ float steps8(const Raw8<T>& raw, float bias, bool soft, int valid, float* dt) {
+  unpack8(raw, dt);
+  float sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float v = dt[j] + bias;
+    dt[j] = j < valid ? (soft ? softplus(v) : v) : 0.f;
+    sum += dt[j];
+  }
+  return sum;
+}
+
+// A wave's values of four channels' states: [channel][S] in LDS as in memory,
+// so entry e belongs to channel e / S.
+template <typename T>
+__device__ __forceinline__ int64_t state_at(const ScanArgs<T>& a, const Place& p, int64_t outer) {
+  return (outer * a.D + p.d0) * a.S;
+}
+
+// ENDS: only what the segment makes of a zero state, and its sum of dt.
+template <typename T, int NB, bool ENDS>
+__global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
+  extern __shared__ float lds[];
+  const Place p = place(a);
+  const int S = a.S, rows = ENDS ? S : 2 * S, lane = p.lane, row = p.row, tl = p.tl;
+  const int len = seq_len(a.lengths, p.n, a.L);
+  const int c0 = p.seg * a.seg_chunks, c1 = c0 + a.seg_chunks < a.chunks ? c0 + a.seg_chunks : a.chunks;
+  const int used = (len + kChunk - 1) / kChunk, cend = used < c1 ? used : c1;
+  float* bc = lds;
+  float* hs = lds + 2 * rows * kChunk + p.wave * 8 * S;
+  float* as = hs + 4 * S;
+  const int held = (p.left < 4 ? p.left : 4) * S;  // entries of channels that exist
+  for (int e = lane; e < 4 * S; e += 64) {
+    float A2 = 0.f, h = 0.f;
+    if (e < held) {
+      A2 = kLog2e * a.A[state_at(a, p, 0) + e];
+      if (!ENDS) {
+        if (a.initial) h = a.initial[state_at(a, p, p.n) + e];
+        for (int k = 0; k < p.seg; ++k) {
+          const int64_t at = int64_t(p.n) * a.segs + k;
+          h = __builtin_fmaf(exp2_fast(A2 * a.end_dt[at * a.D + p.d0 + e / S]), h, a.ends[state_at(a, p, at) + e]);
+        }
+      }
+    }
+    as[e] = A2;
+    hs[e] = h;
+  }
+  const T* up = a.u + p.n * a.u_n + p.d * a.u_d + tl * 8;
+  const T* dp = a.delta + p.n * a.delta_n + p.d * a.delta_d + tl * 8;
+  const T* zp = a.z ? a.z + p.n * a.z_n + p.d * a.z_d + tl * 8 : nullptr;
+  const T* Bp = a.B + p.n * a.B_n + p.g * a.B_g;
+  const T* Cp = a.C + p.n * a.C_n + p.g * a.C_g;
+  const float skip = a.Dskip ? a.Dskip[p.d] : 0.f, bias = a.bias ? a.bias[p.d] : 0.f;
+  T* op = ENDS ? nullptr : a.out + (int64_t(p.n) * a.D + p.d) * a.L + tl * 8;
+  float total = 0.f;
+  Stage<T, NB> st;
+  Raw8<T> ru = {}, rd = {}, rz = {};
+  if (c0 < cend) {
+    st.load(Bp, a.B_s, Cp, a.C_s, S, rows, c0 * kChunk, len);
+    ru = load8(up + c0 * kChunk, len - c0 * kChunk - tl * 8);
+    rd = load8(dp + c0 * kChunk, len - c0 * kChunk - tl * 8);
+    st.store(bc, rows);
+  }
+  __syncthreads();
+  for (int c = c0; c < cend; ++c) {
+    const int t0 = c * kChunk, valid = len - t0 - tl * 8;
+    const float* cur = bc + ((c - c0) & 1) * rows * kChunk;
+    if (!ENDS && a.checkpoints) {
+      float* to = a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + c);
+      for (int e = lane; e < held; e += 64) to[e] = hs[e];
+    }
+    float dt[8], x[8], y[8];
+    const float sum = steps8(rd, bias, a.softplus, valid, dt);
+    unpack8(ru, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      y[j] = skip * x[j];
+      x[j] *= dt[j];
+    }
+    if (c + 1 < cend) {
+      st.load(Bp, a.B_s, Cp, a.C_s, S, rows, t0 + kChunk, len);
+      ru = load8(up + t0 + kChunk, valid - kChunk);
+      rd = load8(dp + t0 + kChunk, valid - kChunk);
+    }
+    if (!ENDS && zp) rz = load8(zp + t0, valid);
+#pragma unroll 1
+    for (int s = 0; s < S; ++s) {
+      const float A2 = as[row * S + s], in = hs[row * S + s];
+      float b[8], w[8];
+      lds8(cur + s * kChunk, tl, b);
+      float H = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        w[j] = exp2_fast(dt[j] * A2);
+        b[j] *= x[j];
+        H = j ? __builtin_fmaf(w[j], H, b[j]) : b[j];
+      }
+      float h = scan_row(H, exp2_fast(sum * A2), in, tl);
+      if (ENDS) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h = __builtin_fmaf(w[j], h, b[j]);
+      } else {
+        float cc[8];
+        lds8(cur + (S + s) * kChunk, tl, cc);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          h = __builtin_fmaf(w[j], h, b[j]);
+          y[j] = __builtin_fmaf(h, cc[j], y[j]);
+        }
+      }
+      if (tl == 15) hs[row * S + s] = h;
+    }
+    total += sum;
+    if (!ENDS && p.ok) {
+      if (zp) {
+        float z[8];
+        unpack8(rz, z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] *= z[j] * sigmoid(z[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = j < valid ? y[j] : 0.f;
+      store8(op + t0, a.L - t0 - tl * 8, y);
+    }
+    if (c + 1 < cend) st.store(bc + ((c + 1 - c0) & 1) * rows * kChunk, rows);
+    __syncthreads();
+  }
+  if (ENDS) {
+    const int64_t at = int64_t(p.n) * a.segs + p.seg;
+    for (int e = lane; e < held; e += 64) a.ends[state_at(a, p, at) + e] = hs[e];
+    total = row_sum(total);
+    if (tl == 15 && p.ok) a.end_dt[at * a.D + p.d] = total;
+    return;
+  }
+  if (a.final_state && p.seg == a.segs - 1) {
+    float* to = a.final_state + state_at(a, p, p.n);
+    for (int e = lane; e < held; e += 64) to[e] = hs[e];
+  }
+  if (p.ok) {  // (chunks behind the end)
+    const float zero[8] = {};
+    for (int c = c0 > used ? c0 : used; c < c1; ++c) store8(op + c * kChunk, a.L - c * kChunk - tl * 8, zero);
+  }
+}
+
+// Sums sixteen values over the four rows: lane (row, tl) gets, of position tl,
+// values 0-3, 4-7 of lo in rows 0, 1 and of hi in rows 2, 3.
+__device__ __forceinline__ f32x4 sum_rows(const float* lo, const float* hi) {
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(lo[j]), __float_as_uint(hi[j]), false, false);
+    v[j] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  f32x4 o;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[j]), __float_as_uint(v[j + 4]), false, false);
+    o[j] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return o;
+}
+
+// Backward.  With e(t) the gradient of h(t) and r(t) = a(t) e(t) what goes on to
+// h(t-1):
+//
+//   e(t) = dy(t) C(t) + r(t+1)        (r behind the end: dfinal_state)
+//   dC = sum_d dy h,  dB = sum_d e x,  dx = sum_s e B,  k = r h(t-1)
+//   ddt = u dx + sum_s A k,  dA = sum k dt,  du = dt dx + Dskip dy
+//
+// The walk is from right to left.  In a chunk the states come again from the
+// checkpoint (the forward pass's scan), then the gradients by the same scan the
+// other way; nothing of a chunk but eight steps' sums outlives a state.  dB and
+// dC are sums over channels: over a wave's four by permlane swaps, over the
+// workgroup's waves through LDS (two states at a time), over workgroups and
+// segments by scan_sum_kernel from `part_bc`, always in the same order.
+// ENDS: only r of the segment alone at its left end, and its sum of dt.
+template <typename T, int NB, bool GATE, bool ENDS>
+__global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
+  extern __shared__ float lds[];
+  const Place p = place(a);
+  const int S = a.S, rows = ENDS ? S : 2 * S, lane = p.lane, row = p.row, tl = p.tl, nw = blockDim.x >> 6;
+  const int len = seq_len(a.lengths, p.n, a.L);
+  const int c0 = p.seg * a.seg_chunks, c1 = c0 + a.seg_chunks < a.chunks ? c0 + a.seg_chunks : a.chunks;
+  const int used = (len + kChunk - 1) / kChunk, cend = used < c1 ? used : c1;
+  float* bc = lds;                                         // B then C (ENDS: C)
+  float* ex = bc + rows * kChunk;                          // [2][kBatch][waves][256]
+  float* as = ex + (ENDS ? 0 : 2 * kBatch * nw * 256) + p.wave * 16 * S;
+  float *rs = as + 4 * S, *hs = rs + 4 * S, *dAs = hs + 4 * S;
+  const int held = (p.left < 4 ? p.left : 4) * S;
+  for (int e = lane; e < 4 * S; e += 64) {
+    float A2 = 0.f, r = 0.f;
+    if (e < held) {
+      A2 = kLog2e * a.A[state_at(a, p, 0) + e];
+      if (!ENDS) {
+        if (a.dfinal) r = a.dfinal[state_at(a, p, p.n) + e];
+        for (int k = a.segs - 1; k > p.seg; --k) {
+          const int64_t at = int64_t(p.n) * a.segs + k;
+          r = __builtin_fmaf(exp2_fast(A2 * a.end_dt[at * a.D + p.d0 + e / S]), r, a.ends[state_at(a, p, at) + e]);
+        }
+      }
+    }
+    as[e] = A2;
+    rs[e] = r;
+    dAs[e] = 0.f;
+  }
+  const T* up = a.u + p.n * a.u_n + p.d * a.u_d + tl * 8;
+  const T* dp = a.delta + p.n * a.delta_n + p.d * a.delta_d + tl * 8;
+  const T* zp = GATE ? a.z + p.n * a.z_n + p.d * a.z_d + tl * 8 : nullptr;
+  const T* gp = a.dout + p.n * a.dout_n + p.d * a.dout_d + tl * 8;
+  const T* Bp = a.B + p.n * a.B_n + p.g * a.B_g;
+  const T* Cp = a.C + p.n * a.C_n + p.g * a.C_g;
+  const float skip = a.Dskip ? a.Dskip[p.d] : 0.f, bias = a.bias ? a.bias[p.d] : 0.f;
+  const int64_t at_row = (int64_t(p.n) * a.D + p.d) * a.L + tl * 8;
+  float total = 0.f, dD = 0.f, dbias = 0.f;
+  Stage<T, NB> st;
+  Raw8<T> ru = {}, rd = {}, rz = {}, rg = {};
+  float ck[4];  // the chunk's checkpoint: entries lane, lane + 64, ...
+  auto fetch = [&](int c) {
+    const int t0 = c * kChunk, valid = len - t0 - tl * 8;
+    if (ENDS)
+      st.load(Cp, a.C_s, Cp, a.C_s, S, rows, t0, len);
+    else
+      st.load(Bp, a.B_s, Cp, a.C_s, S, rows, t0, len);
+    if (!ENDS) ru = load8(up + t0, valid);
+    rd = load8(dp + t0, valid);
+    rg = load8(gp + t0, valid);
+    if (GATE) rz = load8(zp + t0, valid);
+    if (!ENDS) {
+      const float* from = a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + c);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int e = lane + k * 64;
+        ck[k] = e < held ? from[e] : 0.f;
+      }
+    }
+  };
+  if (c0 < cend) fetch(cend - 1);
+  for (int c = cend - 1; c >= c0; --c) {
+    const int t0 = c * kChunk, valid = len - t0 - tl * 8;
+    __syncthreads();  // (the chunk before has been read)
+    st.store(bc, rows);
+    if (!ENDS) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (lane + k * 64 < 4 * S) hs[lane + k * 64] = ck[k];
+    }
+    float dt[8], x[8], u[8], g[8], z[8], dy[8], dx[8], ddt[8], y[8];
+    const float sum = steps8(rd, bias, a.softplus, valid, dt);
+    float raw[8];
+    if (!ENDS) {
+      unpack8(ru, u);
+      unpack8(rd, raw);
+    }
+    unpack8(rg, g);
+    if (GATE) unpack8(rz, z);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      dy[j] = GATE ? g[j] * (z[j] * sigmoid(z[j])) : g[j];
+      if (!ENDS) {
+        x[j] = dt[j] * u[j];
+        dx[j] = ddt[j] = 0.f;
+        y[j] = skip * u[j];
+      }
+    }
+    __syncthreads();
+    if (c > c0) fetch(c - 1);
+    if (ENDS) {
+#pragma unroll 1
+      for (int s = 0; s < S; ++s) {
+        const float A2 = as[row * S + s], in = rs[row * S + s];
+        float w[8], cc[8], R = 0.f;
+        lds8(bc + s * kChunk, tl, cc);
+#pragma unroll
+        for (int j = 7; j >= 0; --j) {
+          w[j] = exp2_fast(dt[j] * A2);
+          R = w[j] * __builtin_fmaf(dy[j], cc[j], R);
+        }
+        float r = scan_row_back(R, exp2_fast(sum * A2), in, tl);
+#pragma unroll
+        for (int j = 7; j >= 0; --j) r = w[j] * __builtin_fmaf(dy[j], cc[j], r);
+        if (tl == 0) rs[row * S + s] = r;
+      }
+      total += sum;
+      continue;
+    }
+    for (int s0 = 0; s0 < S; s0 += kBatch) {
+      float* exb = ex + (s0 / kBatch & 1) * kBatch * nw * 256;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int s = s0 + i;
+        if (s < S) {
+          const float A2 = as[row * S + s];
+          float b[8], cc[8], w[8], h[8], dB[8], dC[8];
+          lds8(bc + s * kChunk, tl, b);
+          lds8(bc + (S + s) * kChunk, tl, cc);
+          float H = 0.f, R = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            w[j] = exp2_fast(dt[j] * A2);
+            H = __builtin_fmaf(w[j], H, x[j] * b[j]);
+          }
+#pragma unroll
+          for (int j = 7; j >= 0; --j) R = w[j] * __builtin_fmaf(dy[j], cc[j], R);
+          const float P = exp2_fast(sum * A2);
+          const float before = scan_row(H, P, hs[row * S + s], tl);
+          float r = scan_row_back(R, P, rs[row * S + s], tl);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            h[j] = __builtin_fmaf(w[j], j ? h[j ? j - 1 : 0] : before, x[j] * b[j]);
+            if (GATE) y[j] = __builtin_fmaf(h[j], cc[j], y[j]);
+          }
+          float dA = 0.f;
+#pragma unroll
+          for (int j = 7; j >= 0; --j) {
+            const float e = __builtin_fmaf(dy[j], cc[j], r);
+            dC[j] = dy[j] * h[j];
+            dB[j] = e * x[j];
+            dx[j] = __builtin_fmaf(e, b[j], dx[j]);
+            r = w[j] * e;
+            const float k = r * (j ? h[j ? j - 1 : 0] : before);
+            ddt[j] = __builtin_fmaf(A2, k, ddt[j]);
+            dA = __builtin_fmaf(k, dt[j], dA);
+          }
+          if (!p.ok) {  // (the clamped channel's terms are not this row's)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) dB[j] = dC[j] = 0.f;
+          }
+          *reinterpret_cast<f32x4*>(exb + (i * nw + p.wave) * 256 + lane * 4) = sum_rows(dB, dC);
+          dA = row_sum(dA);
+          if (tl == 15) dAs[row * S + s] += dA;
+          if (tl == 0) rs[row * S + s] = r;
+        }
+      }
+      __syncthreads();
+      float* to = a.part_bc + ((int64_t(p.n) * a.G + p.g) * a.blks + p.blk) * S * 2 * a.chunks * kChunk;
+      for (int o = threadIdx.x; o < kBatch * 256; o += blockDim.x) {
+        const int i = o >> 8, q = o & 255, s = s0 + i;
+        if (s < S) {
+          float v = 0.f;
+          for (int w = 0; w < nw; ++w) v += exb[(i * nw + w) * 256 + q];
+          to[((int64_t(s) * 2 + (q >> 7)) * a.chunks + c) * kChunk + (q & 127)] = v;
+        }
+      }
+    }
+    if (p.ok) {
+      float o[8], od[8], oz[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool in = j < valid;
+        const float dd = __builtin_fmaf(dx[j], u[j], kLn2 * ddt[j]);
+        od[j] = in ? (a.softplus ? dd * sigmoid(raw[j] + bias) : dd) : 0.f;
+        o[j] = in ? __builtin_fmaf(dx[j], dt[j], skip * dy[j]) : 0.f;
+        dD += in ? dy[j] * u[j] : 0.f;
+        dbias += od[j];
+        if (GATE) {
+          const float sg = sigmoid(z[j]);
+          oz[j] = in ? g[j] * y[j] * (sg * (1.f + z[j] * (1.f - sg))) : 0.f;
+        }
+      }
+      const int room = a.L - t0 - tl * 8;
+      store8(a.du + at_row + t0, room, o);
+      store8(a.ddelta + at_row + t0, room, od);
+      if (GATE) store8(a.dz + at_row + t0, room, oz);
+    }
+  }
+  const int64_t at = int64_t(p.n) * a.segs + p.seg;
+  if (ENDS) {
+    for (int e = lane; e < held; e += 64) a.ends[state_at(a, p, at) + e] = rs[e];
+    total = row_sum(total);
+    if (tl == 15 && p.ok) a.end_dt[at * a.D + p.d] = total;
+    return;
+  }
+  for (int e = lane; e < held; e += 64) {
+    a.part_A[state_at(a, p, at) + e] = dAs[e];
+    if (a.dinitial && p.seg == 0) a.dinitial[state_at(a, p, p.n) + e] = rs[e];
+  }
+  dD = row_sum(dD), dbias = row_sum(dbias);
+  if (!p.ok) return;
+  if (tl == 15) {
+    float* to = a.part_D + (at * a.D + p.d) * 2;
+    to[0] = dD, to[1] = dbias;
+  }
+  const float zero[8] = {};
+  for (int c = c0 > used ? c0 : used; c < c1; ++c) {
+    const int t0 = c * kChunk, room = a.L - t0 - tl * 8;
+    store8(a.du + at_row + t0, room, zero);
+    store8(a.ddelta + at_row + t0, room, zero);
+    if (GATE) store8(a.dz + at_row + t0, room, zero);
+  }
+}
+
+// Adds the backward pass's parts in order.  The first `bc_wgs` workgroups: four
+// steps of dB or dC a thread, over the channel blocks; the others: an element of
+// dA, dDskip or ddelta_bias, over sequences and segments.
+template <typename T>
+__global__ __launch_bounds__(256) void scan_sum_kernel(const ScanArgs<T> a, uint32_t bc_wgs) {
+  if (blockIdx.x < bc_wgs) {
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    const int quads = a.chunks * (kChunk / 4);
+    const int64_t r = i / quads;  // (n, g, s, which)
+    if (r >= int64_t(a.N) * a.G * a.S * 2) return;
+    const int q = int(i - r * quads), c = q / 32, t = c * kChunk + (q & 15) * 8 + (q >> 4 & 1) * 4;
+    if (t >= a.L) return;
+    const int which = int(r & 1);
+    const int64_t ng = r / (2 * a.S), ngs = r >> 1;
+    const int s = int(ngs - ng * a.S), len = seq_len(a.lengths, int(ng / a.G), a.L);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (c * kChunk < len) {
+      const int64_t step = int64_t(a.S) * 2 * a.chunks * kChunk;
+      const float* from = a.part_bc + ng * a.blks * step + (int64_t(s) * 2 + which) * a.chunks * kChunk + int64_t(q) * 4;
+      for (int b = 0; b < a.blks; ++b) v += *reinterpret_cast<const f32x4*>(from + b * step);
+    }
+    T* to = (which ? a.dC : a.dB) + ngs * a.L + t;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (t + j < a.L) to[j] = from_f<T>(t + j < len ? v[j] : 0.f);
+    return;
+  }
+  const int64_t i = int64_t(blockIdx.x - bc_wgs) * 256 + threadIdx.x, states = int64_t(a.D) * a.S;
+  const int parts = a.N * a.segs;
+  if (i < states) {
+    float v = 0.f;
+    for (int k = 0; k < parts; ++k) v += a.part_A[k * states + i];
+    a.dA[i] = v;
+  } else if (i < states + int64_t(a.D) * 2) {
+    const int64_t e = i - states;
+    float v = 0.f;
+    for (int k = 0; k < parts; ++k) v += a.part_D[k * int64_t(a.D) * 2 + e];
+    float* to = e & 1 ? a.dbias : a.dD;
+    if (to) to[e >> 1] = v;
+  }
+}
+
+// One token: four states a lane, the lanes of a channel next to one another, so
+// the states go through as they lie in memory.
+template <typename T>
+struct StepArgs {
+  int D, S, per, G, softplus;
+  uint32_t rows;  // N D
+  int shift;      // log2 of the lanes of a channel
+  int64_t u_n, u_d, delta_n, delta_d, z_n, z_d, B_n, B_g, B_s, C_n, C_g, C_s;
+  const T *u, *delta, *z, *B, *C;
+  const float *A, *Dskip, *bias, *initial;
+  T* out;
+  float* final_state;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
+  const uint64_t i = uint64_t(blockIdx.x) * 256 + threadIdx.x;
+  const uint32_t r = uint32_t(i >> a.shift), rc = r < a.rows ? r : a.rows - 1;
+  const int s0 = int(i & ((1u << a.shift) - 1)) * 4;
+  const uint32_t n = rc / uint32_t(a.D);
+  const int d = int(rc - n * a.D), g = d / a.per;
+  const float u = to_f(a.u[n * a.u_n + d * a.u_d]);
+  float dt = to_f(a.delta[n * a.delta_n + d * a.delta_d]) + (a.bias ? a.bias[d] : 0.f);
+  if (a.softplus) dt = softplus(dt);
+  const float x = dt * u;
+  const float* from = a.initial + int64_t(rc) * a.S + s0;
+  float* to = a.final_state + int64_t(rc) * a.S + s0;
+  const float* A = a.A + int64_t(d) * a.S + s0;
+  const T* B = a.B + n * a.B_n + g * a.B_g + s0 * a.B_s;
+  const T* C = a.C + n * a.C_n + g * a.C_g + s0 * a.C_s;
+  float y = 0.f;
+  float h[4] = {}, A4[4] = {};
+  const int m = a.S - s0 < 4 ? a.S - s0 : 4;
+  if (m == 4) {
+    __builtin_memcpy(h, from, 16);
+    __builtin_memcpy(A4, A, 16);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (j < m) h[j] = from[j], A4[j] = A[j];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (j < m) {
+      h[j] = __builtin_fmaf(exp2_fast(kLog2e * A4[j] * dt), h[j], x * to_f(B[j * a.B_s]));
+      y = __builtin_fmaf(to_f(C[j * a.C_s]), h[j], y);
+    }
+  }
+  if (r < a.rows) {
+    if (m == 4) {
+      __builtin_memcpy(to, h, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+        if (j < m) to[j] = h[j];
+    }
+  }
+  for (int k = 1; k < 1 << a.shift; k <<= 1) y += __shfl_xor(y, k);
+  if (s0 == 0 && r < a.rows) {
+    if (a.Dskip) y = __builtin_fmaf(a.Dskip[d], u, y);
+    if (a.z) {
+      const float z = to_f(a.z[n * a.z_n + d * a.z_d]);
+      y *= z * sigmoid(z);
+    }
+    a.out[r] = from_f<T>(y);
+  }
+}
+
+struct Shape {
+  int per, waves, blks, segs, seg_chunks, chunks;
+  int64_t wgs;
+};
+// `few`: below that many waves the length is cut.
+Shape shape_of(const seq_scan_t& p, bool bwd) {
+  Shape s = {};
+  s.per = p.D / p.G;
+  s.waves = s.per > 16 ? 8 : 4;
+  s.blks = int(ceil_div(s.per, s.waves * 4));
+  s.chunks = int(ceil_div(p.L, kChunk));
+  const int64_t wgs = int64_t(p.N) * p.G * s.blks, waves = wgs * s.waves;
+  int64_t segs = 1;
+  if (waves <= (bwd ? 1024 : 512)) segs = ceil_div(2048, waves);
+  if (segs > s.chunks / 2) segs = s.chunks / 2;
+  if (segs < 1) segs = 1;
+  s.seg_chunks = int(ceil_div(s.chunks, segs));
+  s.segs = int(ceil_div(s.chunks, s.seg_chunks));
+  s.wgs = wgs * s.segs;
+  return s;
+}
+int64_t pad4(int64_t n) { return (n + 3) / 4 * 4; }
+int64_t ends_floats(const seq_scan_t& p, const Shape& s) {
+  return s.segs > 1 ? pad4(int64_t(p.N) * s.segs * p.D * p.S) + pad4(int64_t(p.N) * s.segs * p.D) : 0;
+}
+
+template <typename T>
+ScanArgs<T> args_of(const seq_scan_t& p, const Shape& s) {
+  ScanArgs<T> a = {};
+  a.N = p.N, a.D = p.D, a.L = p.L, a.S = p.S, a.G = p.G, a.per = s.per, a.softplus = p.delta_softplus;
+  a.blks = s.blks, a.segs = s.segs, a.seg_chunks = s.seg_chunks, a.chunks = s.chunks;
+  a.u_n = p.u_n, a.u_d = p.u_d, a.delta_n = p.delta_n, a.delta_d = p.delta_d, a.z_n = p.z_n, a.z_d = p.z_d;
+  a.dout_n = p.dout_n, a.dout_d = p.dout_d;
+  a.B_n = p.B_n, a.B_g = p.B_g, a.B_s = p.B_s, a.C_n = p.C_n, a.C_g = p.C_g, a.C_s = p.C_s;
+  const auto t = [](const void* v) { return static_cast<const T*>(v); };
+  const auto w = [](void* v) { return static_cast<T*>(v); };
+  a.u = t(p.u), a.delta = t(p.delta), a.z = t(p.z), a.B = t(p.B), a.C = t(p.C);
+  a.A = p.A, a.Dskip = p.Dskip, a.bias = p.delta_bias, a.initial = p.initial_state, a.lengths = p.lengths;
+  a.out = w(p.out), a.final_state = p.final_state, a.checkpoints = p.checkpoints;
+  a.dout = t(p.dout), a.dfinal = p.dfinal_state;
+  a.du = w(p.du), a.ddelta = w(p.ddelta), a.dz = w(p.dz), a.dB = w(p.dB), a.dC = w(p.dC);
+  a.dA = p.dA, a.dD = p.dDskip, a.dbias = p.ddelta_bias, a.dinitial = p.dinitial_state;
+  return a;
+}
+
+template <typename K, typename A>
+int launch(K kernel, int64_t wgs, int threads, int64_t lds, hipStream_t s, const A& a) {
+  if (lds > 65536 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                         hipFuncAttributeMaxDynamicSharedMemorySize, int(lds)) != hipSuccess)
+    return CONV_EHIP;
+  kernel<<<dim3(uint32_t(wgs)), threads, uint32_t(lds), s>>>(a);
+  return hipGetLastError() == hipSuccess ? CONV_OK : CONV_EHIP;
+}
+// Staging loads of 16 bytes (fp32: 32) a thread holds for the next chunk.
+template <typename F>
+int with_loads(int rows, int waves, F f) {
+  const int64_t nb = ceil_div(rows * 16, waves * 64);
+  if (nb <= 1) return f(std::integral_constant<int, 1>{});
+  if (nb <= 2) return f(std::integral_constant<int, 2>{});
+  if (nb <= 4) return f(std::integral_constant<int, 4>{});
+  return f(std::integral_constant<int, 8>{});
+}
+
+template <typename T>
+int fwd(const seq_scan_t& p, hipStream_t st) {
+  const Shape s = shape_of(p, false);
+  if (s.wgs * s.waves * 64 > kMaxThreads) return CONV_ERANGE;
+  if (s.segs > 1 && !p.workspace) return CONV_ENULL;
+  if (s.segs > 1 && p.workspace_bytes < scan_fwd_workspace(p)) return CONV_ESCRATCH;
+  ScanArgs<T> a = args_of<T>(p, s);
+  a.ends = static_cast<float*>(p.workspace);
+  a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * p.D * p.S);
+  const auto lds = [&](int rows) { return (2 * int64_t(rows) * kChunk + s.waves * 8 * p.S) * 4; };
+  if (s.segs > 1) {
+    const int rc = with_loads(p.S, s.waves, [&](auto nb) {
+      return launch(scan_fwd_kernel<T, decltype(nb)::value, true>, s.wgs, s.waves * 64, lds(p.S), st, a);
+    });
+    if (rc != CONV_OK) return rc;
+  }
+  return with_loads(2 * p.S, s.waves, [&](auto nb) {
+    return launch(scan_fwd_kernel<T, decltype(nb)::value, false>, s.wgs, s.waves * 64, lds(2 * p.S), st, a);
+  });
+}
+
+template <typename T>
+int bwd(const seq_scan_t& p, hipStream_t st) {
+  const Shape s = shape_of(p, true);
+  const int64_t bc_wgs = ceil_div(int64_t(p.N) * p.G * p.S * 2 * s.chunks * (kChunk / 4), 256);
+  const int64_t sum_wgs = bc_wgs + ceil_div(int64_t(p.D) * (p.S + 2), 256);
+  if (s.wgs * s.waves * 64 > kMaxThreads || sum_wgs * 256 > kMaxThreads) return CONV_ERANGE;
+  if (!p.workspace) return CONV_ENULL;
+  if (p.workspace_bytes < scan_bwd_workspace(p)) return CONV_ESCRATCH;
+  ScanArgs<T> a = args_of<T>(p, s);
+  a.part_bc = static_cast<float*>(p.workspace);
+  a.part_A = a.part_bc + int64_t(p.N) * p.G * s.blks * p.S * 2 * s.chunks * kChunk;
+  a.part_D = a.part_A + pad4(int64_t(p.N) * s.segs * p.D * p.S);
+  a.ends = a.part_D + pad4(int64_t(p.N) * s.segs * p.D * 2);
+  a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * p.D * p.S);
+  const auto lds = [&](int rows, bool ends) {
+    return (int64_t(rows) * kChunk + (ends ? 0 : 2 * kBatch * s.waves * 256) + s.waves * 16 * p.S) * 4;
+  };
+  const bool gate = p.z != nullptr;
+  int rc = CONV_OK;
+  if (s.segs > 1) {
+    rc = with_loads(p.S, s.waves, [&](auto nb) {
+      constexpr int NB = decltype(nb)::value;
+      return launch(gate ? scan_bwd_kernel<T, NB, true, true> : scan_bwd_kernel<T, NB, false, true>, s.wgs,
+                    s.waves * 64, lds(p.S, true), st, a);
+    });
+    if (rc != CONV_OK) return rc;
+  }
+  rc = with_loads(2 * p.S, s.waves, [&](auto nb) {
+    constexpr int NB = decltype(nb)::value;
+    return launch(gate ? scan_bwd_kernel<T, NB, true, false> : scan_bwd_kernel<T, NB, false, false>, s.wgs,
+                  s.waves * 64, lds(2 * p.S, false), st, a);
+  });
+  if (rc != CONV_OK) return rc;
+  scan_sum_kernel<T><<<dim3(uint32_t(sum_wgs)), 256, 0, st>>>(a, uint32_t(bc_wgs));
+  return hipGetLastError() == hipSuccess ? CONV_OK : CONV_EHIP;
+}
+
+template <typename T>
+int step(const seq_scan_t& p, hipStream_t st) {
+  StepArgs<T> a = {};
+  a.D = p.D, a.S = p.S, a.G = p.G, a.per = p.D / p.G, a.softplus = p.delta_softplus;
+  while ((4 << a.shift) < p.S) ++a.shift;
+  const int64_t rows = int64_t(p.N) * p.D, wgs = ceil_div(rows << a.shift, 256);
+  if (wgs * 256 > kMaxThreads) return CONV_ERANGE;
+  a.rows = uint32_t(rows);
+  a.u_n = p.u_n, a.u_d = p.u_d, a.delta_n = p.delta_n, a.delta_d = p.delta_d, a.z_n = p.z_n, a.z_d = p.z_d;
+  a.B_n = p.B_n, a.B_g = p.B_g, a.B_s = p.B_s, a.C_n = p.C_n, a.C_g = p.C_g, a.C_s = p.C_s;
+  const auto t = [](const void* v) { return static_cast<const T*>(v); };
+  a.u = t(p.u), a.delta = t(p.delta), a.z = t(p.z), a.B = t(p.B), a.C = t(p.C);
+  a.A = p.A, a.Dskip = p.Dskip, a.bias = p.delta_bias, a.initial = p.initial_state;
+  a.out = static_cast<T*>(p.out), a.final_state = p.final_state;
+  scan_step_kernel<T><<<dim3(uint32_t(wgs)), 256, 0, st>>>(a);
+  return hipGetLastError() == hipSuccess ? CONV_OK : CONV_EHIP;
+}
+}  // namespace
+
+int64_t scan_fwd_workspace(const seq_scan_t& p) {
+  return ends_floats(p, shape_of(p, false)) * int64_t(sizeof(float));
+}
+int64_t scan_bwd_workspace(const seq_scan_t& p) {
+  const Shape s = shape_of(p, true);
+  const int64_t rows = int64_t(p.N) * s.segs * p.D;
+  return (int64_t(p.N) * p.G * s.blks * p.S * 2 * s.chunks * kChunk + pad4(rows * p.S) + pad4(rows * 2) +
+          ends_floats(p, s)) * int64_t(sizeof(float));
+}
+int launch_scan_fwd(const seq_scan_t& p, void* stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  return p.dtype == CONV_DTYPE_BF16 ? fwd<bf16>(p, s) : fwd<float>(p, s);
+}
+int launch_scan_bwd(const seq_scan_t& p, void* stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  return p.dtype == CONV_DTYPE_BF16 ? bwd<bf16>(p, s) : bwd<float>(p, s);
+}
+int launch_scan_step(const seq_scan_t& p, void* stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  return p.dtype == CONV_DTYPE_BF16 ? step<bf16>(p, s) : step<float>(p, s);
+}
+
+}  // namespace seqops
