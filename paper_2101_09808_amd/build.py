@@ -1,4 +1,5 @@
-"""Build the HIP library ``libconvfwd.so`` in-tree for gfx950 with hipcc.
+"""Build the HIP library ``libconvfwd.so`` in-tree for gfx950 with hipcc, and
+the Python module ``_seq.so`` on it.
 
     python -m paper_2101_09808_amd.build
 """
@@ -11,6 +12,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libconvfwd.so")
+SEQ = os.path.join(PKG, "_seq.so")
 INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 
 SOURCES = ("conv_kernels.hip", "split_kernels.hip", "seq_scan.hip", "seq_norm.hip", "seq_conv.hip",
@@ -38,6 +40,29 @@ def _compile(src):
     return out, msgs
 
 
+def _build_python(verbose):
+    """The module _seq (host code on torch's and Python's headers): its calls go to LIB."""
+    import sysconfig
+
+    import torch
+
+    torch_dir = os.path.dirname(torch.__file__)
+    tmp = SEQ + ".tmp%d" % os.getpid()
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-shared", "-Wall", "-DUSE_ROCM",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *HOST_FLAGS, "-I", INCLUDE,
+           "-isystem", os.path.join(torch_dir, "include"),
+           "-isystem", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "seq_python.cpp"), "-o", tmp,
+           "-L", PKG, "-lconvfwd", "-L", os.path.join(torch_dir, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu",
+           "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}{r.stderr}")
+    if verbose and (r.stdout or r.stderr):
+        print(r.stdout + r.stderr)
+    os.replace(tmp, SEQ)
+
+
 def build(verbose=False):
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
@@ -53,6 +78,7 @@ def build(verbose=False):
     if r.returncode != 0:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}{r.stderr}")
     os.replace(tmp, LIB)
+    _build_python(verbose)
     return LIB
 
 
