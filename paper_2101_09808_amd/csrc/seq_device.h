@@ -68,6 +68,15 @@ __device__ __forceinline__ Raw8<T> load8(const T* p, int valid) {
   return r;
 }
 
+// The same bits, which the compiler has to unpack again instead of holding what
+// it unpacked before: registers.
+template <typename T>
+__device__ __forceinline__ Raw8<T> again(Raw8<T> r) {
+#pragma unroll
+  for (int i = 0; i < int(2 * sizeof(T)); ++i) asm volatile("" : "+v"(r.w[i]));
+  return r;
+}
+
 template <typename T>
 __device__ __forceinline__ void unpack8(const Raw8<T>& r, float* v) {
 #pragma unroll
@@ -121,20 +130,18 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + exp2_fast(-kLog2e * x)); }
 
 // log(1 + exp(x)) = max(x, 0) + log1p(e), e = exp(-|x|) in (0, 1], and
-// log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3, by its series in s^2 (the
-// ninth term is below 2e-8 of the first): steps of 1e-3 keep their digits.
+// log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3: steps of 1e-3 keep their
+// digits.  2 artanh(s) / s is a polynomial in q = s^2, interpolated at the
+// Chebyshev nodes of [0, 1/9] (within 4e-9 of it).
 __device__ __forceinline__ float softplus(float x) {
   const float e = exp2_fast(-kLog2e * __builtin_fabsf(x));
   const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
-  float p = 1.f / 15.f;
-  p = __builtin_fmaf(p, q, 1.f / 13.f);
-  p = __builtin_fmaf(p, q, 1.f / 11.f);
-  p = __builtin_fmaf(p, q, 1.f / 9.f);
-  p = __builtin_fmaf(p, q, 1.f / 7.f);
-  p = __builtin_fmaf(p, q, 1.f / 5.f);
-  p = __builtin_fmaf(p, q, 1.f / 3.f);
-  p = __builtin_fmaf(p, q, 1.f);
-  return __builtin_fmaxf(x, 0.f) + 2.f * s * p;
+  float p = 0.2815778f;
+  p = __builtin_fmaf(p, q, 0.27965158f);
+  p = __builtin_fmaf(p, q, 0.40024596f);
+  p = __builtin_fmaf(p, q, 0.6666632f);
+  p = __builtin_fmaf(p, q, 2.f);
+  return __builtin_fmaf(s, p, __builtin_fmaxf(x, 0.f));
 }
 
 // DPP moves within a row of 16 lanes or the wave.  `old` is what lanes without

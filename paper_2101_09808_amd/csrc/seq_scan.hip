@@ -27,13 +27,13 @@ namespace seqops {
 namespace {
 
 constexpr int kChunk = SEQ_SCAN_CHUNK;  // 16 lanes of 8 steps
-constexpr int kBatch = 2;               // states between two exchanges of dB and dC
 
 template <typename T>
 struct ScanArgs {
   int N, D, L, S, G, per;  // per: channels of a group
   int softplus;
   int blks, segs, seg_chunks, chunks;
+  int batch;  // backward: states between two exchanges of dB and dC, a power of 2
   int64_t u_n, u_d, delta_n, delta_d, z_n, z_d, dout_n, dout_d, B_n, B_g, B_s, C_n, C_g, C_s;
   const T *u, *delta, *z, *B, *C;
   const float *A, *Dskip, *bias, *initial;
@@ -77,10 +77,10 @@ __device__ __forceinline__ Place place(const ScanArgs<T>& a) {
   return p;
 }
 
-// A chunk of B (and C) in LDS: a state's steps in two runs of 64, the first and
-// the last four steps of every lane, so that a lane's reads are whole 16-byte
-// banks next to its neighbours'.
-template <typename T, int NB>
+// B (and C) of the steps that a workgroup works on, TS a lane, in LDS: a
+// state's steps in runs of 64, four of every lane, so that a lane's reads are
+// whole 16-byte banks next to its neighbours'.
+template <typename T, int TS, int NB>
 struct Stage {
   Raw8<T> raw[NB];
   // rows 0..S-1 are first's states, the others second's
@@ -88,49 +88,60 @@ struct Stage {
                                        int rows, int t0, int len) {
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
-      const int i = threadIdx.x + k * blockDim.x, r = i >> 4, t = t0 + (i & 15) * 8;
+      const int i = threadIdx.x + k * blockDim.x, r = i / (2 * TS), t = t0 + i % (2 * TS) * 8;
       if (r < rows) raw[k] = load8((r < S ? first + r * first_s : second + (r - S) * second_s) + t, len - t);
     }
   }
   __device__ __forceinline__ void store(float* lds, int rows) const {
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
-      const int i = threadIdx.x + k * blockDim.x, r = i >> 4;
+      const int i = threadIdx.x + k * blockDim.x, r = i / (2 * TS), e = i % (2 * TS);
       if (r < rows) {
         float v[8];
         unpack8(raw[k], v);
-        float* at = lds + r * kChunk + (i & 15) * 4;
+        float* at = lds + r * (16 * TS) + (TS == 8 ? e * 4 : (e & 1) * 128 + (e >> 1) * 4);
         *reinterpret_cast<f32x4*>(at) = f32x4{v[0], v[1], v[2], v[3]};
         *reinterpret_cast<f32x4*>(at + 64) = f32x4{v[4], v[5], v[6], v[7]};
       }
     }
   }
 };
-__device__ __forceinline__ void lds8(const float* lds, int tl, float* v) {
-  const f32x4 lo = *reinterpret_cast<const f32x4*>(lds + tl * 4), hi = *reinterpret_cast<const f32x4*>(lds + 64 + tl * 4);
+template <int TS>
+__device__ __forceinline__ void lds_steps(const float* lds, int tl, float* v) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = lo[j], v[4 + j] = hi[j];
+  for (int k = 0; k < TS / 4; ++k) {
+    const f32x4 q = *reinterpret_cast<const f32x4*>(lds + k * 64 + tl * 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[k * 4 + j] = q[j];
+  }
 }
 
-// The states that reach each lane of a row: H (the lane's steps from zero) and
-// P (their decay) become the state behind the lane; the state before it is
-// returned.  `in` reaches lane 0.
-__device__ __forceinline__ float scan_row(float H, float P, float in, int tl) {
-  H = __builtin_fmaf(P, tl == 0 ? in : 0.f, H);
-  H = __builtin_fmaf(P, dpp0<kRowShr + 1>(H), H), P *= dpp0<kRowShr + 1>(P);
-  H = __builtin_fmaf(P, dpp0<kRowShr + 2>(H), H), P *= dpp0<kRowShr + 2>(P);
-  H = __builtin_fmaf(P, dpp0<kRowShr + 4>(H), H), P *= dpp0<kRowShr + 4>(P);
-  H = __builtin_fmaf(P, dpp0<kRowShr + 8>(H), H);
-  return dpp<kRowShr + 1>(in, H);
+// The states that reach each lane of a row, for two states at once: H (a lane's
+// steps from zero) and P (their decay) are composed in levels of 1, 2, 4 and 8
+// lanes; lane 0 has its incoming state in H already, and a lane without a
+// source adds nothing.  `in` becomes the state before each lane (lane 0: kept).
+// Written as DPP operands, which the compiler makes moves of; a DPP source has
+// to be two instructions old, which the two chains are to one another.
+#define SEQ_SCAN_LEVEL(DIR, K)                                                       \
+  "v_fmac_f32_dpp %0, %0, %2 " DIR ":" #K " row_mask:0xf bank_mask:0xf bound_ctrl:1\n" \
+  "v_fmac_f32_dpp %1, %1, %3 " DIR ":" #K " row_mask:0xf bank_mask:0xf bound_ctrl:1\n"
+#define SEQ_SCAN_DECAY(DIR, K)                                                      \
+  "v_mul_f32_dpp %2, %2, %2 " DIR ":" #K " row_mask:0xf bank_mask:0xf bound_ctrl:1\n" \
+  "v_mul_f32_dpp %3, %3, %3 " DIR ":" #K " row_mask:0xf bank_mask:0xf bound_ctrl:1\n"
+#define SEQ_SCAN_ROW(DIR)                                                                                       \
+  asm volatile("s_nop 1\n" SEQ_SCAN_LEVEL(DIR, 1) SEQ_SCAN_DECAY(DIR, 1) SEQ_SCAN_LEVEL(DIR, 2)                 \
+                   SEQ_SCAN_DECAY(DIR, 2) SEQ_SCAN_LEVEL(DIR, 4) SEQ_SCAN_DECAY(DIR, 4) SEQ_SCAN_LEVEL(DIR, 8)  \
+               "s_nop 0\n"                                                                                      \
+               "v_mov_b32_dpp %4, %0 " DIR ":1 row_mask:0xf bank_mask:0xf\n"                                    \
+               "v_mov_b32_dpp %5, %1 " DIR ":1 row_mask:0xf bank_mask:0xf\n"                                    \
+               "s_nop 1\n"                                                                                      \
+               : "+v"(H0), "+v"(H1), "+v"(P0), "+v"(P1), "+v"(in0), "+v"(in1))
+__device__ __forceinline__ void scan_row(float H0, float H1, float P0, float P1, float& in0, float& in1) {
+  SEQ_SCAN_ROW("row_shr");
 }
-// The same from right to left; `in` reaches lane 15.
-__device__ __forceinline__ float scan_row_back(float H, float P, float in, int tl) {
-  H = __builtin_fmaf(P, tl == 15 ? in : 0.f, H);
-  H = __builtin_fmaf(P, dpp0<kRowShl + 1>(H), H), P *= dpp0<kRowShl + 1>(P);
-  H = __builtin_fmaf(P, dpp0<kRowShl + 2>(H), H), P *= dpp0<kRowShl + 2>(P);
-  H = __builtin_fmaf(P, dpp0<kRowShl + 4>(H), H), P *= dpp0<kRowShl + 4>(P);
-  H = __builtin_fmaf(P, dpp0<kRowShl + 8>(H), H);
-  return dpp<kRowShl + 1>(in, H);
+// The same from right to left (lane 15 keeps its `in`).
+__device__ __forceinline__ void scan_row_back(float H0, float H1, float P0, float P1, float& in0, float& in1) {
+  SEQ_SCAN_ROW("row_shl");
 }
 // A row's sum in its lane 15.
 __device__ __forceinline__ float row_sum(float v) {
@@ -141,17 +152,25 @@ __device__ __forceinline__ float row_sum(float v) {
   return v;
 }
 
-// dt of eight steps (zero behind the end: the state stands still) and its sum.
-template <typename T>
-__device__ __forceinline__ float steps8(const Raw8<T>& raw, float bias, bool soft, int valid, float* dt) {
-  unpack8(raw, dt);
+// dt of a lane's steps and its sum.  `full`: no step of the workgroup's is
+// behind the end; else those have dt = 0 (the state stands still).
+template <typename T, int TS>
+__device__ __forceinline__ float steps(const Raw8<T>* raw, float bias, bool soft, bool full, int valid, float* dt) {
+#pragma unroll
+  for (int k = 0; k < TS / 8; ++k) unpack8(raw[k], dt + 8 * k);
+#pragma unroll
+  for (int j = 0; j < TS; ++j) dt[j] += bias;
+  if (soft) {
+#pragma unroll
+    for (int j = 0; j < TS; ++j) dt[j] = softplus(dt[j]);
+  }
+  if (!full) {
+#pragma unroll
+    for (int j = 0; j < TS; ++j) dt[j] = j < valid ? dt[j] : 0.f;
+  }
   float sum = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float v = dt[j] + bias;
-    dt[j] = j < valid ? (soft ? softplus(v) : v) : 0.f;
-    sum += dt[j];
-  }
+  for (int j = 0; j < TS; ++j) sum += dt[j];
   return sum;
 }
 
@@ -162,128 +181,177 @@ __device__ __forceinline__ int64_t state_at(const ScanArgs<T>& a, const Place& p
   return (outer * a.D + p.d0) * a.S;
 }
 
-// ENDS: only what the segment makes of a zero state, and its sum of dt.
-template <typename T, int NB, bool ENDS>
+// TS steps a lane, 16 TS a pass.  ENDS: only what the segment makes of a zero
+// state, and its sum of dt.
+template <typename T, int TS, int NB, bool ENDS>
 __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
   extern __shared__ float lds[];
+  constexpr int kSteps = 16 * TS, kPer = kSteps / kChunk;  // checkpoints a pass
   const Place p = place(a);
-  const int S = a.S, rows = ENDS ? S : 2 * S, lane = p.lane, row = p.row, tl = p.tl;
+  const int S = a.S, Se = (S + 1) & ~1, rows = ENDS ? S : 2 * S, lane = p.lane, row = p.row, tl = p.tl;
   const int len = seq_len(a.lengths, p.n, a.L);
-  const int c0 = p.seg * a.seg_chunks, c1 = c0 + a.seg_chunks < a.chunks ? c0 + a.seg_chunks : a.chunks;
-  const int used = (len + kChunk - 1) / kChunk, cend = used < c1 ? used : c1;
-  float* bc = lds;
-  float* hs = lds + 2 * rows * kChunk + p.wave * 8 * S;
-  float* as = hs + 4 * S;
-  const int held = (p.left < 4 ? p.left : 4) * S;  // entries of channels that exist
-  for (int e = lane; e < 4 * S; e += 64) {
+  // (a segment is of whole passes)
+  const int first = p.seg * a.seg_chunks * kChunk;
+  const int stop = p.seg == a.segs - 1 ? a.L : first + a.seg_chunks * kChunk, end = len < stop ? len : stop;
+  float* bc = lds;  // [2][rows], a row of zeros behind them
+  float* zeros = bc + 2 * rows * kSteps;
+  float* hs = zeros + kSteps + p.wave * (8 + 4 * (kPer - 1)) * Se;
+  float *as = hs + 4 * Se, *mid = as + 4 * Se;  // mid: states after lane 7
+  const int held = p.left < 4 ? p.left : 4;     // channels that exist
+  for (int e = lane; e < 4 * Se; e += 64) {
+    const int r = e / Se, s = e - r * Se;
     float A2 = 0.f, h = 0.f;
-    if (e < held) {
-      A2 = kLog2e * a.A[state_at(a, p, 0) + e];
+    if (r < held && s < S) {
+      const int64_t at0 = int64_t(r) * S + s;
+      A2 = kLog2e * a.A[state_at(a, p, 0) + at0];
       if (!ENDS) {
-        if (a.initial) h = a.initial[state_at(a, p, p.n) + e];
+        if (a.initial) h = a.initial[state_at(a, p, p.n) + at0];
         for (int k = 0; k < p.seg; ++k) {
           const int64_t at = int64_t(p.n) * a.segs + k;
-          h = __builtin_fmaf(exp2_fast(A2 * a.end_dt[at * a.D + p.d0 + e / S]), h, a.ends[state_at(a, p, at) + e]);
+          h = __builtin_fmaf(exp2_fast(A2 * a.end_dt[at * a.D + p.d0 + r]), h, a.ends[state_at(a, p, at) + at0]);
         }
       }
     }
     as[e] = A2;
     hs[e] = h;
   }
-  const T* up = a.u + p.n * a.u_n + p.d * a.u_d + tl * 8;
-  const T* dp = a.delta + p.n * a.delta_n + p.d * a.delta_d + tl * 8;
-  const T* zp = a.z ? a.z + p.n * a.z_n + p.d * a.z_d + tl * 8 : nullptr;
+  for (int e = threadIdx.x; e < kSteps; e += blockDim.x) zeros[e] = 0.f;
+  // entry e of [channel][S] in memory, from an array of [channel][Se]
+  auto put = [&](float* to, const float* from) {
+    for (int e = lane; e < held * S; e += 64) {
+      const int r = e / S;
+      to[e] = from[e + r * (Se - S)];
+    }
+  };
+  const T* up = a.u + p.n * a.u_n + p.d * a.u_d + tl * TS;
+  const T* dp = a.delta + p.n * a.delta_n + p.d * a.delta_d + tl * TS;
+  const T* zp = a.z ? a.z + p.n * a.z_n + p.d * a.z_d + tl * TS : nullptr;
   const T* Bp = a.B + p.n * a.B_n + p.g * a.B_g;
   const T* Cp = a.C + p.n * a.C_n + p.g * a.C_g;
   const float skip = a.Dskip ? a.Dskip[p.d] : 0.f, bias = a.bias ? a.bias[p.d] : 0.f;
-  T* op = ENDS ? nullptr : a.out + (int64_t(p.n) * a.D + p.d) * a.L + tl * 8;
+  T* op = ENDS ? nullptr : a.out + (int64_t(p.n) * a.D + p.d) * a.L + tl * TS;
   float total = 0.f;
-  Stage<T, NB> st;
-  Raw8<T> ru = {}, rd = {}, rz = {};
-  if (c0 < cend) {
-    st.load(Bp, a.B_s, Cp, a.C_s, S, rows, c0 * kChunk, len);
-    ru = load8(up + c0 * kChunk, len - c0 * kChunk - tl * 8);
-    rd = load8(dp + c0 * kChunk, len - c0 * kChunk - tl * 8);
+  Stage<T, TS, NB> st;
+  Raw8<T> ru[TS / 8] = {}, rd[TS / 8] = {}, rz[TS / 8] = {};
+  auto fetch = [&](const T* from, int t0, Raw8<T>* r) {
+#pragma unroll
+    for (int k = 0; k < TS / 8; ++k) r[k] = load8(from + t0 + 8 * k, len - t0 - tl * TS - 8 * k);
+  };
+  if (first < end) {
+    st.load(Bp, a.B_s, Cp, a.C_s, S, rows, first, len);
+    fetch(up, first, ru);
+    fetch(dp, first, rd);
     st.store(bc, rows);
   }
   __syncthreads();
-  for (int c = c0; c < cend; ++c) {
-    const int t0 = c * kChunk, valid = len - t0 - tl * 8;
-    const float* cur = bc + ((c - c0) & 1) * rows * kChunk;
-    if (!ENDS && a.checkpoints) {
-      float* to = a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + c);
-      for (int e = lane; e < held; e += 64) to[e] = hs[e];
-    }
-    float dt[8], x[8], y[8];
-    const float sum = steps8(rd, bias, a.softplus, valid, dt);
-    unpack8(ru, x);
+  int buf = 0;
+  for (int t0 = first; t0 < end; t0 += kSteps) {
+    const int valid = len - t0 - tl * TS;
+    const float* cur = bc + buf * rows * kSteps;
+    const bool more = t0 + kSteps < end, full = t0 + kSteps <= len;
+    if (!ENDS && a.checkpoints)
+      put(a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + t0 / kChunk), hs);
+    float dt[TS], x[TS], y[TS];
+    const float sum = steps<T, TS>(rd, bias, a.softplus, full, valid, dt);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int k = 0; k < TS / 8; ++k) unpack8(ru[k], x + 8 * k);
+#pragma unroll
+    for (int j = 0; j < TS; ++j) {
       y[j] = skip * x[j];
       x[j] *= dt[j];
     }
-    if (c + 1 < cend) {
-      st.load(Bp, a.B_s, Cp, a.C_s, S, rows, t0 + kChunk, len);
-      ru = load8(up + t0 + kChunk, valid - kChunk);
-      rd = load8(dp + t0 + kChunk, valid - kChunk);
+    if (more) {
+      st.load(Bp, a.B_s, Cp, a.C_s, S, rows, t0 + kSteps, len);
+      fetch(up, t0 + kSteps, ru);
+      fetch(dp, t0 + kSteps, rd);
     }
-    if (!ENDS && zp) rz = load8(zp + t0, valid);
-#pragma unroll 1
-    for (int s = 0; s < S; ++s) {
-      const float A2 = as[row * S + s], in = hs[row * S + s];
-      float b[8], w[8];
-      lds8(cur + s * kChunk, tl, b);
-      float H = 0.f;
+    if (!ENDS && zp) fetch(zp, t0, rz);
+    for (int s = 0; s < S; s += 2) {
+      // (with S odd the last state's pair is of decay 1 and reads zeros)
+      const bool two = s + 1 < S;
+      const float *b0 = cur + s * kSteps, *b1 = two ? b0 + kSteps : zeros;
+      float w[2][TS], b[2][TS], A2[2], in[2], H[2], P[2];
+      lds_steps<TS>(b0, tl, b[0]);
+      lds_steps<TS>(b1, tl, b[1]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        w[j] = exp2_fast(dt[j] * A2);
-        b[j] *= x[j];
-        H = j ? __builtin_fmaf(w[j], H, b[j]) : b[j];
+      for (int i = 0; i < 2; ++i) {
+        A2[i] = as[row * Se + s + i];
+        in[i] = hs[row * Se + s + i];
       }
-      float h = scan_row(H, exp2_fast(sum * A2), in, tl);
-      if (ENDS) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) h = __builtin_fmaf(w[j], h, b[j]);
-      } else {
-        float cc[8];
-        lds8(cur + (S + s) * kChunk, tl, cc);
+      for (int i = 0; i < 2; ++i) P[i] = exp2_fast(sum * A2[i]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          h = __builtin_fmaf(w[j], h, b[j]);
-          y[j] = __builtin_fmaf(h, cc[j], y[j]);
+      for (int j = 0; j < TS; ++j) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          w[i][j] = exp2_fast(dt[j] * A2[i]);
+          b[i][j] *= x[j];
+          H[i] = j ? __builtin_fmaf(w[i][j], H[i], b[i][j]) : b[i][j];
         }
       }
-      if (tl == 15) hs[row * S + s] = h;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) H[i] = __builtin_fmaf(P[i], tl == 0 ? in[i] : 0.f, H[i]);
+      scan_row(H[0], H[1], P[0], P[1], in[0], in[1]);
+      if (ENDS) {
+#pragma unroll
+        for (int j = 0; j < TS; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) in[i] = __builtin_fmaf(w[i][j], in[i], b[i][j]);
+      } else {
+        float c[2][TS];
+        lds_steps<TS>(b0 + S * kSteps, tl, c[0]);
+        lds_steps<TS>(two ? b0 + (S + 1) * kSteps : zeros, tl, c[1]);
+#pragma unroll
+        for (int j = 0; j < TS; ++j) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            in[i] = __builtin_fmaf(w[i][j], in[i], b[i][j]);
+            y[j] = __builtin_fmaf(in[i], c[i][j], y[j]);
+          }
+        }
+      }
+      if (kPer > 1 && !ENDS && tl == 7) mid[row * Se + s] = in[0], mid[row * Se + s + 1] = in[1];
+      if (tl == 15) hs[row * Se + s] = in[0], hs[row * Se + s + 1] = in[1];
     }
     total += sum;
+    if (kPer > 1 && !ENDS && a.checkpoints && t0 + kChunk < end)
+      put(a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + t0 / kChunk + 1), mid);
     if (!ENDS && p.ok) {
-      if (zp) {
-        float z[8];
-        unpack8(rz, z);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] *= z[j] * sigmoid(z[j]);
+      for (int k = 0; k < TS / 8; ++k) {
+        float* yk = y + 8 * k;
+        if (zp) {
+          float z[8];
+          unpack8(rz[k], z);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) yk[j] *= z[j] * sigmoid(z[j]);
+        }
+        if (!full) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) yk[j] = 8 * k + j < valid ? yk[j] : 0.f;
+        }
+        store8(op + t0 + 8 * k, a.L - t0 - tl * TS - 8 * k, yk);
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = j < valid ? y[j] : 0.f;
-      store8(op + t0, a.L - t0 - tl * 8, y);
     }
-    if (c + 1 < cend) st.store(bc + ((c + 1 - c0) & 1) * rows * kChunk, rows);
+    if (more) st.store(bc + (buf ^ 1) * rows * kSteps, rows);
+    buf ^= 1;
     __syncthreads();
   }
   if (ENDS) {
     const int64_t at = int64_t(p.n) * a.segs + p.seg;
-    for (int e = lane; e < held; e += 64) a.ends[state_at(a, p, at) + e] = hs[e];
+    put(a.ends + state_at(a, p, at), hs);
     total = row_sum(total);
     if (tl == 15 && p.ok) a.end_dt[at * a.D + p.d] = total;
     return;
   }
-  if (a.final_state && p.seg == a.segs - 1) {
-    float* to = a.final_state + state_at(a, p, p.n);
-    for (int e = lane; e < held; e += 64) to[e] = hs[e];
-  }
-  if (p.ok) {  // (chunks behind the end)
+  if (a.final_state && p.seg == a.segs - 1) put(a.final_state + state_at(a, p, p.n), hs);
+  if (p.ok) {  // (passes behind the end)
     const float zero[8] = {};
-    for (int c = c0 > used ? c0 : used; c < c1; ++c) store8(op + c * kChunk, a.L - c * kChunk - tl * 8, zero);
+    int t0 = first;
+    if (end > first) t0 += (end - first + kSteps - 1) / kSteps * kSteps;
+    for (; t0 < stop; t0 += kSteps)
+#pragma unroll
+      for (int k = 0; k < TS / 8; ++k) store8(op + t0 + 8 * k, stop - t0 - tl * TS - 8 * k, zero);
   }
 }
 
@@ -323,31 +391,36 @@ template <typename T, int NB, bool GATE, bool ENDS>
 __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
   extern __shared__ float lds[];
   const Place p = place(a);
-  const int S = a.S, rows = ENDS ? S : 2 * S, lane = p.lane, row = p.row, tl = p.tl, nw = blockDim.x >> 6;
+  const int S = a.S, Se = (S + 1) & ~1, rows = ENDS ? S : 2 * S, lane = p.lane, row = p.row, tl = p.tl;
+  const int nw = blockDim.x >> 6, batch = a.batch;
   const int len = seq_len(a.lengths, p.n, a.L);
   const int c0 = p.seg * a.seg_chunks, c1 = c0 + a.seg_chunks < a.chunks ? c0 + a.seg_chunks : a.chunks;
   const int used = (len + kChunk - 1) / kChunk, cend = used < c1 ? used : c1;
-  float* bc = lds;                                         // B then C (ENDS: C)
-  float* ex = bc + rows * kChunk;                          // [2][kBatch][waves][256]
-  float* as = ex + (ENDS ? 0 : 2 * kBatch * nw * 256) + p.wave * 16 * S;
-  float *rs = as + 4 * S, *hs = rs + 4 * S, *dAs = hs + 4 * S;
-  const int held = (p.left < 4 ? p.left : 4) * S;
-  for (int e = lane; e < 4 * S; e += 64) {
+  float* bc = lds;                     // B then C (ENDS: C), a row of zeros behind them
+  float* zeros = bc + rows * kChunk;
+  float* ex = zeros + kChunk;          // [batch][waves][256]
+  float* as = ex + (ENDS ? 0 : batch * nw * 256) + p.wave * (ENDS ? 8 : 16) * Se;
+  float *rs = as + 4 * Se, *hs = rs + 4 * Se, *dAs = hs + 4 * Se;  // (ENDS: the first two)
+  const int held = p.left < 4 ? p.left : 4;
+  for (int e = lane; e < 4 * Se; e += 64) {
+    const int r0 = e / Se, s = e - r0 * Se;
     float A2 = 0.f, r = 0.f;
-    if (e < held) {
-      A2 = kLog2e * a.A[state_at(a, p, 0) + e];
+    if (r0 < held && s < S) {
+      const int64_t at0 = int64_t(r0) * S + s;
+      A2 = kLog2e * a.A[state_at(a, p, 0) + at0];
       if (!ENDS) {
-        if (a.dfinal) r = a.dfinal[state_at(a, p, p.n) + e];
+        if (a.dfinal) r = a.dfinal[state_at(a, p, p.n) + at0];
         for (int k = a.segs - 1; k > p.seg; --k) {
           const int64_t at = int64_t(p.n) * a.segs + k;
-          r = __builtin_fmaf(exp2_fast(A2 * a.end_dt[at * a.D + p.d0 + e / S]), r, a.ends[state_at(a, p, at) + e]);
+          r = __builtin_fmaf(exp2_fast(A2 * a.end_dt[at * a.D + p.d0 + r0]), r, a.ends[state_at(a, p, at) + at0]);
         }
       }
     }
     as[e] = A2;
     rs[e] = r;
-    dAs[e] = 0.f;
+    if (!ENDS) hs[e] = dAs[e] = 0.f;
   }
+  for (int e = threadIdx.x; e < kChunk; e += blockDim.x) zeros[e] = 0.f;
   const T* up = a.u + p.n * a.u_n + p.d * a.u_d + tl * 8;
   const T* dp = a.delta + p.n * a.delta_n + p.d * a.delta_d + tl * 8;
   const T* zp = GATE ? a.z + p.n * a.z_n + p.d * a.z_d + tl * 8 : nullptr;
@@ -356,12 +429,14 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
   const T* Cp = a.C + p.n * a.C_n + p.g * a.C_g;
   const float skip = a.Dskip ? a.Dskip[p.d] : 0.f, bias = a.bias ? a.bias[p.d] : 0.f;
   const int64_t at_row = (int64_t(p.n) * a.D + p.d) * a.L + tl * 8;
+  // (the steps of a row without a channel are all behind its end: they add nothing)
+  const int row_len = p.ok ? len - tl * 8 : 0;
   float total = 0.f, dD = 0.f, dbias = 0.f;
-  Stage<T, NB> st;
+  Stage<T, 8, NB> st;
   Raw8<T> ru = {}, rd = {}, rz = {}, rg = {};
-  float ck[4];  // the chunk's checkpoint: entries lane, lane + 64, ...
+  float ck[4];  // the chunk's checkpoint: entries lane, lane + 64, ... of [channel][S]
   auto fetch = [&](int c) {
-    const int t0 = c * kChunk, valid = len - t0 - tl * 8;
+    const int t0 = c * kChunk, valid = row_len - t0;
     if (ENDS)
       st.load(Cp, a.C_s, Cp, a.C_s, S, rows, t0, len);
     else
@@ -373,134 +448,177 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
     if (!ENDS) {
       const float* from = a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + c);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int e = lane + k * 64;
-        ck[k] = e < held ? from[e] : 0.f;
-      }
+      for (int k = 0; k < 4; ++k)
+        if (lane + k * 64 < held * S) ck[k] = from[lane + k * 64];
     }
   };
+  int ck_at[4];  // where they belong in [channel][Se]
+#pragma unroll
+  for (int k = 0; k < 4; ++k) ck_at[k] = lane + k * 64 + (lane + k * 64) / S * (Se - S);
   if (c0 < cend) fetch(cend - 1);
   for (int c = cend - 1; c >= c0; --c) {
-    const int t0 = c * kChunk, valid = len - t0 - tl * 8;
+    const int t0 = c * kChunk, valid = row_len - t0;
+    const bool full = t0 + kChunk <= len;
     __syncthreads();  // (the chunk before has been read)
     st.store(bc, rows);
     if (!ENDS) {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (lane + k * 64 < 4 * S) hs[lane + k * 64] = ck[k];
+        if (lane + k * 64 < held * S) hs[ck_at[k]] = ck[k];
     }
-    float dt[8], x[8], u[8], g[8], z[8], dy[8], dx[8], ddt[8], y[8];
-    const float sum = steps8(rd, bias, a.softplus, valid, dt);
-    float raw[8];
-    if (!ENDS) {
-      unpack8(ru, u);
-      unpack8(rd, raw);
-    }
-    unpack8(rg, g);
-    if (GATE) unpack8(rz, z);
+    float dt[8], x[8], dy[8], dx[8], ddt[8], y[8];
+    const float sum = steps<T, 8>(&rd, bias, a.softplus, full, valid, dt);
+    const Raw8<T> ku = again(ru), kd = again(rd), kg = again(rg), kz = again(rz);
+    {
+      float z[8], u[8];
+      unpack8(rg, dy);
+      if (GATE) {
+        unpack8(rz, z);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      dy[j] = GATE ? g[j] * (z[j] * sigmoid(z[j])) : g[j];
+        for (int j = 0; j < 8; ++j) dy[j] *= z[j] * sigmoid(z[j]);
+      }
       if (!ENDS) {
-        x[j] = dt[j] * u[j];
-        dx[j] = ddt[j] = 0.f;
-        y[j] = skip * u[j];
+        unpack8(ru, u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          x[j] = dt[j] * u[j];
+          dx[j] = ddt[j] = 0.f;
+          y[j] = skip * u[j];
+        }
       }
     }
     __syncthreads();
     if (c > c0) fetch(c - 1);
-    if (ENDS) {
-#pragma unroll 1
-      for (int s = 0; s < S; ++s) {
-        const float A2 = as[row * S + s], in = rs[row * S + s];
-        float w[8], cc[8], R = 0.f;
-        lds8(bc + s * kChunk, tl, cc);
+    // Two states at a time (with S odd the last one's pair is of decay 1 and
+    // reads zeros), `batch` between two exchanges.
+    for (int s = 0; s < S; s += 2) {
+      const bool two = s + 1 < S;
+      const float* b0 = bc + s * kChunk;
+      const float* q0 = ENDS ? b0 : b0 + S * kChunk;
+      float b[2][8], cc[2][8], w[2][8], A2[2], rin[2], R[2] = {0.f, 0.f}, P[2];
+      lds_steps<8>(q0, tl, cc[0]);
+      lds_steps<8>(two ? q0 + kChunk : zeros, tl, cc[1]);
 #pragma unroll
-        for (int j = 7; j >= 0; --j) {
-          w[j] = exp2_fast(dt[j] * A2);
-          R = w[j] * __builtin_fmaf(dy[j], cc[j], R);
-        }
-        float r = scan_row_back(R, exp2_fast(sum * A2), in, tl);
-#pragma unroll
-        for (int j = 7; j >= 0; --j) r = w[j] * __builtin_fmaf(dy[j], cc[j], r);
-        if (tl == 0) rs[row * S + s] = r;
+      for (int i = 0; i < 2; ++i) {
+        A2[i] = as[row * Se + s + i];
+        rin[i] = rs[row * Se + s + i];
+        P[i] = exp2_fast(sum * A2[i]);
       }
-      total += sum;
-      continue;
-    }
-    for (int s0 = 0; s0 < S; s0 += kBatch) {
-      float* exb = ex + (s0 / kBatch & 1) * kBatch * nw * 256;
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int s = s0 + i;
-        if (s < S) {
-          const float A2 = as[row * S + s];
-          float b[8], cc[8], w[8], h[8], dB[8], dC[8];
-          lds8(bc + s * kChunk, tl, b);
-          lds8(bc + (S + s) * kChunk, tl, cc);
-          float H = 0.f, R = 0.f;
+      for (int j = 7; j >= 0; --j) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            w[j] = exp2_fast(dt[j] * A2);
-            H = __builtin_fmaf(w[j], H, x[j] * b[j]);
-          }
-#pragma unroll
-          for (int j = 7; j >= 0; --j) R = w[j] * __builtin_fmaf(dy[j], cc[j], R);
-          const float P = exp2_fast(sum * A2);
-          const float before = scan_row(H, P, hs[row * S + s], tl);
-          float r = scan_row_back(R, P, rs[row * S + s], tl);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            h[j] = __builtin_fmaf(w[j], j ? h[j ? j - 1 : 0] : before, x[j] * b[j]);
-            if (GATE) y[j] = __builtin_fmaf(h[j], cc[j], y[j]);
-          }
-          float dA = 0.f;
-#pragma unroll
-          for (int j = 7; j >= 0; --j) {
-            const float e = __builtin_fmaf(dy[j], cc[j], r);
-            dC[j] = dy[j] * h[j];
-            dB[j] = e * x[j];
-            dx[j] = __builtin_fmaf(e, b[j], dx[j]);
-            r = w[j] * e;
-            const float k = r * (j ? h[j ? j - 1 : 0] : before);
-            ddt[j] = __builtin_fmaf(A2, k, ddt[j]);
-            dA = __builtin_fmaf(k, dt[j], dA);
-          }
-          if (!p.ok) {  // (the clamped channel's terms are not this row's)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) dB[j] = dC[j] = 0.f;
-          }
-          *reinterpret_cast<f32x4*>(exb + (i * nw + p.wave) * 256 + lane * 4) = sum_rows(dB, dC);
-          dA = row_sum(dA);
-          if (tl == 15) dAs[row * S + s] += dA;
-          if (tl == 0) rs[row * S + s] = r;
+        for (int i = 0; i < 2; ++i) {
+          w[i][j] = exp2_fast(dt[j] * A2[i]);
+          R[i] = w[i][j] * __builtin_fmaf(dy[j], cc[i][j], R[i]);
         }
       }
-      __syncthreads();
-      float* to = a.part_bc + ((int64_t(p.n) * a.G + p.g) * a.blks + p.blk) * S * 2 * a.chunks * kChunk;
-      for (int o = threadIdx.x; o < kBatch * 256; o += blockDim.x) {
-        const int i = o >> 8, q = o & 255, s = s0 + i;
-        if (s < S) {
-          float v = 0.f;
-          for (int w = 0; w < nw; ++w) v += exb[(i * nw + w) * 256 + q];
-          to[((int64_t(s) * 2 + (q >> 7)) * a.chunks + c) * kChunk + (q & 127)] = v;
-        }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) R[i] = __builtin_fmaf(P[i], tl == 15 ? rin[i] : 0.f, R[i]);
+      scan_row_back(R[0], R[1], P[0], P[1], rin[0], rin[1]);
+      if (ENDS) {
+#pragma unroll
+        for (int j = 7; j >= 0; --j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) rin[i] = w[i][j] * __builtin_fmaf(dy[j], cc[i][j], rin[i]);
+        if (tl == 0) rs[row * Se + s] = rin[0], rs[row * Se + s + 1] = rin[1];
+        continue;
       }
-    }
-    if (p.ok) {
-      float o[8], od[8], oz[8];
+      float* exb = ex + (s & (batch - 1)) * nw * 256 + p.wave * 256 + lane * 4;
+      float h[2][8], hin[2], H[2] = {0.f, 0.f}, dA[2] = {0.f, 0.f};
+      lds_steps<8>(b0, tl, b[0]);
+      lds_steps<8>(two ? b0 + kChunk : zeros, tl, b[1]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) hin[i] = hs[row * Se + s + i];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const bool in = j < valid;
-        const float dd = __builtin_fmaf(dx[j], u[j], kLn2 * ddt[j]);
-        od[j] = in ? (a.softplus ? dd * sigmoid(raw[j] + bias) : dd) : 0.f;
-        o[j] = in ? __builtin_fmaf(dx[j], dt[j], skip * dy[j]) : 0.f;
-        dD += in ? dy[j] * u[j] : 0.f;
-        dbias += od[j];
-        if (GATE) {
-          const float sg = sigmoid(z[j]);
-          oz[j] = in ? g[j] * y[j] * (sg * (1.f + z[j] * (1.f - sg))) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          h[i][j] = x[j] * b[i][j];
+          H[i] = __builtin_fmaf(w[i][j], H[i], h[i][j]);
         }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        P[i] = exp2_fast(sum * A2[i]);
+        H[i] = __builtin_fmaf(P[i], tl == 0 ? hin[i] : 0.f, H[i]);
+      }
+      scan_row(H[0], H[1], P[0], P[1], hin[0], hin[1]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          h[i][j] = __builtin_fmaf(w[i][j], j ? h[i][j ? j - 1 : 0] : hin[i], h[i][j]);
+          if (GATE) y[j] = __builtin_fmaf(h[i][j], cc[i][j], y[j]);
+        }
+      }
+      float dB[2][8], dC[2][8];
+#pragma unroll
+      for (int j = 7; j >= 0; --j) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float e = __builtin_fmaf(dy[j], cc[i][j], rin[i]);
+          dC[i][j] = dy[j] * h[i][j];
+          dB[i][j] = e * x[j];
+          dx[j] = __builtin_fmaf(e, b[i][j], dx[j]);
+          rin[i] = w[i][j] * e;
+          const float k = rin[i] * (j ? h[i][j ? j - 1 : 0] : hin[i]);
+          ddt[j] = __builtin_fmaf(A2[i], k, ddt[j]);
+          dA[i] = __builtin_fmaf(k, dt[j], dA[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        *reinterpret_cast<f32x4*>(exb + i * nw * 256) = sum_rows(dB[i], dC[i]);
+        dA[i] = row_sum(dA[i]);
+      }
+      if (tl == 15) dAs[row * Se + s] += dA[0], dAs[row * Se + s + 1] += dA[1];
+      if (tl == 0) rs[row * Se + s] = rin[0], rs[row * Se + s + 1] = rin[1];
+      if ((s + 2 & (batch - 1)) && s + 2 < S) continue;
+      const int s0 = s & -batch;
+      __syncthreads();
+      float* to = a.part_bc + ((int64_t(p.n) * a.G + p.g) * a.blks + p.blk) * S * 2 * a.chunks * kChunk;
+      for (int o = threadIdx.x; o < batch * 128; o += blockDim.x) {
+        const int i = o >> 7, q = (o & 127) * 2;
+        if (s0 + i < S) {
+          f32x2 v = {0.f, 0.f};
+          for (int w2 = 0; w2 < nw; ++w2) v += *reinterpret_cast<const f32x2*>(ex + (i * nw + w2) * 256 + q);
+          *reinterpret_cast<f32x2*>(to + ((int64_t(s0 + i) * 2 + (q >> 7)) * a.chunks + c) * kChunk + (q & 127)) = v;
+        }
+      }
+      if (s + 2 < S) __syncthreads();  // (the next batch overwrites these)
+    }
+    total += sum;
+    if (ENDS) continue;
+    if (p.ok) {
+      float u[8], raw[8], o[8], od[8], oz[8];
+      unpack8(ku, u);
+      unpack8(kd, raw);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        od[j] = __builtin_fmaf(dx[j], u[j], kLn2 * ddt[j]);
+        // softplus's slope exp(v) / (1 + exp(v)) = exp(v - softplus(v))
+        if (a.softplus) od[j] *= exp2_fast(kLog2e * (raw[j] + bias - dt[j]));
+        o[j] = __builtin_fmaf(dx[j], dt[j], skip * dy[j]);
+      }
+      if (GATE) {
+        float g[8], z[8];
+        unpack8(kg, g);
+        unpack8(kz, z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float sg = sigmoid(z[j]);
+          oz[j] = g[j] * y[j] * (sg * (1.f + z[j] * (1.f - sg)));
+        }
+      }
+      if (!full) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j >= valid) o[j] = od[j] = oz[j] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        dD = __builtin_fmaf(dy[j], u[j], dD);
+        dbias += od[j];
       }
       const int room = a.L - t0 - tl * 8;
       store8(a.du + at_row + t0, room, o);
@@ -509,16 +627,17 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
     }
   }
   const int64_t at = int64_t(p.n) * a.segs + p.seg;
+  const auto put = [&](float* to, const float* from) {
+    for (int e = lane; e < held * S; e += 64) to[e] = from[e + e / S * (Se - S)];
+  };
   if (ENDS) {
-    for (int e = lane; e < held; e += 64) a.ends[state_at(a, p, at) + e] = rs[e];
+    put(a.ends + state_at(a, p, at), rs);
     total = row_sum(total);
     if (tl == 15 && p.ok) a.end_dt[at * a.D + p.d] = total;
     return;
   }
-  for (int e = lane; e < held; e += 64) {
-    a.part_A[state_at(a, p, at) + e] = dAs[e];
-    if (a.dinitial && p.seg == 0) a.dinitial[state_at(a, p, p.n) + e] = rs[e];
-  }
+  put(a.part_A + state_at(a, p, at), dAs);
+  if (a.dinitial && p.seg == 0) put(a.dinitial + state_at(a, p, p.n), rs);
   dD = row_sum(dD), dbias = row_sum(dbias);
   if (!p.ok) return;
   if (tl == 15) {
@@ -645,21 +764,23 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
 
 struct Shape {
   int per, waves, blks, segs, seg_chunks, chunks;
+  int steps;  // a lane's in a pass (backward: 8)
   int64_t wgs;
 };
-// `few`: below that many waves the length is cut.
 Shape shape_of(const seq_scan_t& p, bool bwd) {
   Shape s = {};
   s.per = p.D / p.G;
   s.waves = s.per > 16 ? 8 : 4;
   s.blks = int(ceil_div(s.per, s.waves * 4));
   s.chunks = int(ceil_div(p.L, kChunk));
+  s.steps = !bwd && p.L > 512 && p.S <= 32 ? 16 : 8;
+  const int per = s.steps / 8;  // chunks a pass
   const int64_t wgs = int64_t(p.N) * p.G * s.blks, waves = wgs * s.waves;
   int64_t segs = 1;
   if (waves <= (bwd ? 1024 : 512)) segs = ceil_div(2048, waves);
-  if (segs > s.chunks / 2) segs = s.chunks / 2;
+  if (segs > s.chunks / (2 * per)) segs = s.chunks / (2 * per);
   if (segs < 1) segs = 1;
-  s.seg_chunks = int(ceil_div(s.chunks, segs));
+  s.seg_chunks = int(ceil_div(ceil_div(s.chunks, segs), per) * per);
   s.segs = int(ceil_div(s.chunks, s.seg_chunks));
   s.wgs = wgs * s.segs;
   return s;
@@ -696,16 +817,24 @@ int launch(K kernel, int64_t wgs, int threads, int64_t lds, hipStream_t s, const
   kernel<<<dim3(uint32_t(wgs)), threads, uint32_t(lds), s>>>(a);
   return hipGetLastError() == hipSuccess ? CONV_OK : CONV_EHIP;
 }
-// Staging loads of 16 bytes (fp32: 32) a thread holds for the next chunk.
+// Staging loads of 16 bytes (fp32: 32) a thread holds for the next pass.
 template <typename F>
-int with_loads(int rows, int waves, F f) {
-  const int64_t nb = ceil_div(rows * 16, waves * 64);
+int with_loads(int rows, int steps, int waves, F f) {
+  const int64_t nb = ceil_div(rows * steps * 2, waves * 64);
   if (nb <= 1) return f(std::integral_constant<int, 1>{});
   if (nb <= 2) return f(std::integral_constant<int, 2>{});
   if (nb <= 4) return f(std::integral_constant<int, 4>{});
   return f(std::integral_constant<int, 8>{});
 }
 
+template <typename T, int TS, bool ENDS>
+int fwd_pass(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
+  const int rows = ENDS ? p.S : 2 * p.S;
+  const int64_t lds = ((2 * rows + 1) * int64_t(16 * TS) + s.waves * (6 + TS / 4) * ((p.S + 1) & ~1)) * 4;
+  return with_loads(rows, TS, s.waves, [&](auto nb) {
+    return launch(scan_fwd_kernel<T, TS, decltype(nb)::value, ENDS>, s.wgs, s.waves * 64, lds, st, a);
+  });
+}
 template <typename T>
 int fwd(const seq_scan_t& p, hipStream_t st) {
   const Shape s = shape_of(p, false);
@@ -715,18 +844,32 @@ int fwd(const seq_scan_t& p, hipStream_t st) {
   ScanArgs<T> a = args_of<T>(p, s);
   a.ends = static_cast<float*>(p.workspace);
   a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * p.D * p.S);
-  const auto lds = [&](int rows) { return (2 * int64_t(rows) * kChunk + s.waves * 8 * p.S) * 4; };
   if (s.segs > 1) {
-    const int rc = with_loads(p.S, s.waves, [&](auto nb) {
-      return launch(scan_fwd_kernel<T, decltype(nb)::value, true>, s.wgs, s.waves * 64, lds(p.S), st, a);
-    });
+    const int rc = s.steps == 16 ? fwd_pass<T, 16, true>(p, s, a, st) : fwd_pass<T, 8, true>(p, s, a, st);
     if (rc != CONV_OK) return rc;
   }
-  return with_loads(2 * p.S, s.waves, [&](auto nb) {
-    return launch(scan_fwd_kernel<T, decltype(nb)::value, false>, s.wgs, s.waves * 64, lds(2 * p.S), st, a);
-  });
+  return s.steps == 16 ? fwd_pass<T, 16, false>(p, s, a, st) : fwd_pass<T, 8, false>(p, s, a, st);
 }
 
+// As many as LDS holds beside what S states need: an exchange is two barriers.
+int batch_of(int S) { return S > 32 ? 4 : S > 16 ? 8 : 16; }
+template <typename T, bool GATE, bool ENDS>
+int bwd_pass(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
+  const int rows = ENDS ? p.S : 2 * p.S, Se = (p.S + 1) & ~1;
+  const int64_t lds =
+      ((rows + 1) * int64_t(kChunk) + (ENDS ? 0 : a.batch * s.waves * 256) + s.waves * (ENDS ? 8 : 16) * Se) * 4;
+  return with_loads(rows, 8, s.waves, [&](auto nb) {
+    return launch(scan_bwd_kernel<T, decltype(nb)::value, GATE, ENDS>, s.wgs, s.waves * 64, lds, st, a);
+  });
+}
+template <typename T, bool GATE>
+int bwd_passes(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
+  if (s.segs > 1) {
+    const int rc = bwd_pass<T, GATE, true>(p, s, a, st);
+    if (rc != CONV_OK) return rc;
+  }
+  return bwd_pass<T, GATE, false>(p, s, a, st);
+}
 template <typename T>
 int bwd(const seq_scan_t& p, hipStream_t st) {
   const Shape s = shape_of(p, true);
@@ -736,29 +879,13 @@ int bwd(const seq_scan_t& p, hipStream_t st) {
   if (!p.workspace) return CONV_ENULL;
   if (p.workspace_bytes < scan_bwd_workspace(p)) return CONV_ESCRATCH;
   ScanArgs<T> a = args_of<T>(p, s);
+  a.batch = batch_of(p.S);
   a.part_bc = static_cast<float*>(p.workspace);
   a.part_A = a.part_bc + int64_t(p.N) * p.G * s.blks * p.S * 2 * s.chunks * kChunk;
   a.part_D = a.part_A + pad4(int64_t(p.N) * s.segs * p.D * p.S);
   a.ends = a.part_D + pad4(int64_t(p.N) * s.segs * p.D * 2);
   a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * p.D * p.S);
-  const auto lds = [&](int rows, bool ends) {
-    return (int64_t(rows) * kChunk + (ends ? 0 : 2 * kBatch * s.waves * 256) + s.waves * 16 * p.S) * 4;
-  };
-  const bool gate = p.z != nullptr;
-  int rc = CONV_OK;
-  if (s.segs > 1) {
-    rc = with_loads(p.S, s.waves, [&](auto nb) {
-      constexpr int NB = decltype(nb)::value;
-      return launch(gate ? scan_bwd_kernel<T, NB, true, true> : scan_bwd_kernel<T, NB, false, true>, s.wgs,
-                    s.waves * 64, lds(p.S, true), st, a);
-    });
-    if (rc != CONV_OK) return rc;
-  }
-  rc = with_loads(2 * p.S, s.waves, [&](auto nb) {
-    constexpr int NB = decltype(nb)::value;
-    return launch(gate ? scan_bwd_kernel<T, NB, true, false> : scan_bwd_kernel<T, NB, false, false>, s.wgs,
-                  s.waves * 64, lds(2 * p.S, false), st, a);
-  });
+  const int rc = p.z ? bwd_passes<T, true>(p, s, a, st) : bwd_passes<T, false>(p, s, a, st);
   if (rc != CONV_OK) return rc;
   scan_sum_kernel<T><<<dim3(uint32_t(sum_wgs)), 256, 0, st>>>(a, uint32_t(bc_wgs));
   return hipGetLastError() == hipSuccess ? CONV_OK : CONV_EHIP;
