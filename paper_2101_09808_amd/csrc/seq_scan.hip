@@ -33,6 +33,7 @@ struct ScanArgs {
   int N, D, L, S, G, per;  // per: channels of a group
   int softplus;
   int blks, segs, seg_chunks, chunks;
+  int run_segs, run_first;  // the segments that a launch works on
   int batch;  // backward: states between two exchanges of dB and dC, a power of 2
   int64_t u_n, u_d, delta_n, delta_d, z_n, z_d, dout_n, dout_d, B_n, B_g, B_s, C_n, C_g, C_s;
   const T *u, *delta, *z, *B, *C;
@@ -50,37 +51,37 @@ struct ScanArgs {
   float *part_A, *part_D;  // [N][segs][D][S], [N][segs][D][2] (Dskip, delta_bias)
 };
 
-// Where a thread stands: wave of four channels, a row of sixteen lanes each.
+// Where a thread stands: a wave of RW channels, 64 / RW lanes each.
 struct Place {
   int lane, wave, row, tl;
   int n, g, blk, seg;
   int d0;    // the wave's first channel
-  int left;  // how many of its four there are (none: 0 or less)
+  int held;  // how many of its channels there are (may be none)
   int d;     // the row's channel; one that exists, if its own does not
   bool ok;
 };
-template <typename T>
+template <int RW, typename T>
 __device__ __forceinline__ Place place(const ScanArgs<T>& a) {
   Place p;
   p.lane = threadIdx.x & 63;
   p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  p.row = p.lane >> 4, p.tl = p.lane & 15;
+  p.row = p.lane / (64 / RW), p.tl = p.lane % (64 / RW);
   uint32_t b = blockIdx.x;
   p.blk = int(b % a.blks), b /= a.blks;
   p.g = int(b % a.G), b /= a.G;
-  p.seg = int(b % a.segs), p.n = int(b / a.segs);
-  const int cw = (p.blk * int(blockDim.x >> 6) + p.wave) * 4;
-  p.left = a.per - cw;
+  p.seg = int(b % a.run_segs) + a.run_first, p.n = int(b / a.run_segs);
+  const int cw = (p.blk * int(blockDim.x >> 6) + p.wave) * RW, left = a.per - cw;
+  p.held = left < 0 ? 0 : left < RW ? left : RW;
   p.d0 = p.g * a.per + cw;
-  p.ok = p.row < p.left;
+  p.ok = p.row < left;
   p.d = p.ok ? p.d0 + p.row : p.g * a.per + a.per - 1;
   return p;
 }
 
-// B (and C) of the steps that a workgroup works on, TS a lane, in LDS: a
-// state's steps in runs of 64, four of every lane, so that a lane's reads are
-// whole 16-byte banks next to its neighbours'.
-template <typename T, int TS, int NB>
+// B (and C) of the steps that a workgroup works on, TS for each of the LN lanes
+// of a channel, in LDS: a state's steps in runs of 4 LN, four of every lane, so
+// that a lane's reads are whole 16-byte banks next to its neighbours'.
+template <typename T, int LN, int TS, int NB>
 struct Stage {
   Raw8<T> raw[NB];
   // rows 0..S-1 are first's states, the others second's
@@ -88,60 +89,71 @@ struct Stage {
                                        int rows, int t0, int len) {
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
-      const int i = threadIdx.x + k * blockDim.x, r = i / (2 * TS), t = t0 + i % (2 * TS) * 8;
+      const int i = threadIdx.x + k * blockDim.x, r = i / (LN * TS / 8), t = t0 + i % (LN * TS / 8) * 8;
       if (r < rows) raw[k] = load8((r < S ? first + r * first_s : second + (r - S) * second_s) + t, len - t);
     }
   }
   __device__ __forceinline__ void store(float* lds, int rows) const {
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
-      const int i = threadIdx.x + k * blockDim.x, r = i / (2 * TS), e = i % (2 * TS);
+      const int i = threadIdx.x + k * blockDim.x, r = i / (LN * TS / 8), e = i % (LN * TS / 8);
       if (r < rows) {
         float v[8];
         unpack8(raw[k], v);
-        float* at = lds + r * (16 * TS) + (TS == 8 ? e * 4 : (e & 1) * 128 + (e >> 1) * 4);
+        float* at = lds + r * (LN * TS) + (TS == 8 ? e * 4 : (e & 1) * (8 * LN) + (e >> 1) * 4);
         *reinterpret_cast<f32x4*>(at) = f32x4{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4*>(at + 64) = f32x4{v[4], v[5], v[6], v[7]};
+        *reinterpret_cast<f32x4*>(at + 4 * LN) = f32x4{v[4], v[5], v[6], v[7]};
       }
     }
   }
 };
-template <int TS>
+template <int LN, int TS>
 __device__ __forceinline__ void lds_steps(const float* lds, int tl, float* v) {
 #pragma unroll
   for (int k = 0; k < TS / 4; ++k) {
-    const f32x4 q = *reinterpret_cast<const f32x4*>(lds + k * 64 + tl * 4);
+    const f32x4 q = *reinterpret_cast<const f32x4*>(lds + k * 4 * LN + tl * 4);
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[k * 4 + j] = q[j];
   }
 }
 
-// The states that reach each lane of a row, for two states at once: H (a lane's
-// steps from zero) and P (their decay) are composed in levels of 1, 2, 4 and 8
-// lanes; lane 0 has its incoming state in H already, and a lane without a
-// source adds nothing.  `in` becomes the state before each lane (lane 0: kept).
+// The states that reach each lane, for two states at once: H (a lane's steps
+// from zero; lane 0 has its incoming state in them) and P (their decay) are
+// composed in levels of 1, 2, 4 and 8 lanes, then over two and four rows where
+// a channel has the whole wave.  A lane without a source is left as it is.  H
+// becomes the state behind each lane, `in` the one before it (lane 0: kept).
 // Written as DPP operands, which the compiler makes moves of; a DPP source has
 // to be two instructions old, which the two chains are to one another.
-#define SEQ_SCAN_LEVEL(DIR, K)                                                       \
-  "v_fmac_f32_dpp %0, %0, %2 " DIR ":" #K " row_mask:0xf bank_mask:0xf bound_ctrl:1\n" \
-  "v_fmac_f32_dpp %1, %1, %3 " DIR ":" #K " row_mask:0xf bank_mask:0xf bound_ctrl:1\n"
-#define SEQ_SCAN_DECAY(DIR, K)                                                      \
-  "v_mul_f32_dpp %2, %2, %2 " DIR ":" #K " row_mask:0xf bank_mask:0xf bound_ctrl:1\n" \
-  "v_mul_f32_dpp %3, %3, %3 " DIR ":" #K " row_mask:0xf bank_mask:0xf bound_ctrl:1\n"
-#define SEQ_SCAN_ROW(DIR)                                                                                       \
-  asm volatile("s_nop 1\n" SEQ_SCAN_LEVEL(DIR, 1) SEQ_SCAN_DECAY(DIR, 1) SEQ_SCAN_LEVEL(DIR, 2)                 \
-                   SEQ_SCAN_DECAY(DIR, 2) SEQ_SCAN_LEVEL(DIR, 4) SEQ_SCAN_DECAY(DIR, 4) SEQ_SCAN_LEVEL(DIR, 8)  \
-               "s_nop 0\n"                                                                                      \
-               "v_mov_b32_dpp %4, %0 " DIR ":1 row_mask:0xf bank_mask:0xf\n"                                    \
-               "v_mov_b32_dpp %5, %1 " DIR ":1 row_mask:0xf bank_mask:0xf\n"                                    \
-               "s_nop 1\n"                                                                                      \
-               : "+v"(H0), "+v"(H1), "+v"(P0), "+v"(P1), "+v"(in0), "+v"(in1))
-__device__ __forceinline__ void scan_row(float H0, float H1, float P0, float P1, float& in0, float& in1) {
-  SEQ_SCAN_ROW("row_shr");
+#define SEQ_DPP2(OP, X, Y, CTRL)                \
+  OP " %" #X ", %" #X ", %2 " CTRL "\n" OP " %" #Y ", %" #Y ", %3 " CTRL "\n"
+#define SEQ_LEVEL(CTRL) SEQ_DPP2("v_fmac_f32_dpp", 0, 1, CTRL) SEQ_DPP2("v_mul_f32_dpp", 2, 3, CTRL)
+#define SEQ_ROW(DIR, K) DIR ":" #K " row_mask:0xf bank_mask:0xf"
+#define SEQ_ROW_LEVELS(DIR) \
+  "s_nop 1\n" SEQ_LEVEL(SEQ_ROW(DIR, 1)) SEQ_LEVEL(SEQ_ROW(DIR, 2)) SEQ_LEVEL(SEQ_ROW(DIR, 4))
+#define SEQ_SHIFT(CTRL)                                   \
+  "s_nop 0\n"                                             \
+  "v_mov_b32_dpp %4, %0 " CTRL " row_mask:0xf bank_mask:0xf\n" \
+  "v_mov_b32_dpp %5, %1 " CTRL " row_mask:0xf bank_mask:0xf\n" \
+  "s_nop 1\n"
+#define SEQ_SCAN_OPERANDS "+v"(H[0]), "+v"(H[1]), "+v"(P[0]), "+v"(P[1]), "+v"(in[0]), "+v"(in[1])
+template <int LN>
+__device__ __forceinline__ void scan_lanes(float* H, float* P, float* in) {
+  if constexpr (LN == 16)
+    asm volatile(SEQ_ROW_LEVELS("row_shr") SEQ_DPP2("v_fmac_f32_dpp", 0, 1, SEQ_ROW("row_shr", 8))
+                     SEQ_SHIFT("row_shr:1")
+                 : SEQ_SCAN_OPERANDS);
+  else
+    asm volatile(SEQ_ROW_LEVELS("row_shr") SEQ_LEVEL(SEQ_ROW("row_shr", 8))
+                     SEQ_LEVEL("row_bcast:15 row_mask:0xa bank_mask:0xf")
+                         SEQ_DPP2("v_fmac_f32_dpp", 0, 1, "row_bcast:31 row_mask:0xc bank_mask:0xf")
+                             SEQ_SHIFT("wave_shr:1")
+                 : SEQ_SCAN_OPERANDS);
 }
-// The same from right to left (lane 15 keeps its `in`).
-__device__ __forceinline__ void scan_row_back(float H0, float H1, float P0, float P1, float& in0, float& in1) {
-  SEQ_SCAN_ROW("row_shl");
+// The same from right to left (lane 15 keeps its `in`), rows of sixteen.
+__device__ __forceinline__ void scan_lanes_back(float* H, float* P, float* in) {
+  asm volatile(SEQ_ROW_LEVELS("row_shl") SEQ_DPP2("v_fmac_f32_dpp", 0, 1, SEQ_ROW("row_shl", 8))
+                   SEQ_SHIFT("row_shl:1")
+               : SEQ_SCAN_OPERANDS);
 }
 // A row's sum in its lane 15.
 __device__ __forceinline__ float row_sum(float v) {
@@ -150,6 +162,20 @@ __device__ __forceinline__ float row_sum(float v) {
   v += dpp0<kRowShr + 4>(v);
   v += dpp0<kRowShr + 8>(v);
   return v;
+}
+
+// h (or a gradient) as the segments [from, to) in turn leave it; `at` is the
+// state's place in a segment's `ends`, d its channel.
+template <typename T>
+__device__ __forceinline__ float through(const ScanArgs<T>& a, int n, int from, int to, int step, int64_t at, int d,
+                                         float A2, float h) {
+  const int64_t first = int64_t(n) * a.segs + from;
+  const float *dt = a.end_dt + first * a.D + d, *end = a.ends + first * a.D * a.S + at;
+  const int64_t dt_step = int64_t(step) * a.D, end_step = dt_step * a.S;
+#pragma unroll 4
+  for (int k = from; k != to; k += step, dt += dt_step, end += end_step)
+    h = __builtin_fmaf(exp2_fast(A2 * *dt), h, *end);
+  return h;
 }
 
 // dt of a lane's steps and its sum.  `full`: no step of the workgroup's is
@@ -181,35 +207,32 @@ __device__ __forceinline__ int64_t state_at(const ScanArgs<T>& a, const Place& p
   return (outer * a.D + p.d0) * a.S;
 }
 
-// TS steps a lane, 16 TS a pass.  ENDS: only what the segment makes of a zero
-// state, and its sum of dt.
-template <typename T, int TS, int NB, bool ENDS>
+// RW channels a wave, LN = 64 / RW lanes each; TS steps a lane, LN TS a pass.
+// ENDS: only what the segment makes of a zero state, and its sum of dt.
+template <typename T, int RW, int TS, int NB, bool ENDS>
 __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
   extern __shared__ float lds[];
-  constexpr int kSteps = 16 * TS, kPer = kSteps / kChunk;  // checkpoints a pass
-  const Place p = place(a);
+  constexpr int LN = 64 / RW, kSteps = LN * TS;
+  constexpr int kPer = ENDS ? 1 : kSteps / kChunk, kLanes = kChunk / TS;  // checkpoints a pass, lanes to one
+  const Place p = place<RW>(a);
   const int S = a.S, Se = (S + 1) & ~1, rows = ENDS ? S : 2 * S, lane = p.lane, row = p.row, tl = p.tl;
-  const int len = seq_len(a.lengths, p.n, a.L);
+  const int len = seq_len(a.lengths, p.n, a.L), held = p.held;
   // (a segment is of whole passes)
   const int first = p.seg * a.seg_chunks * kChunk;
   const int stop = p.seg == a.segs - 1 ? a.L : first + a.seg_chunks * kChunk, end = len < stop ? len : stop;
   float* bc = lds;  // [2][rows], a row of zeros behind them
   float* zeros = bc + 2 * rows * kSteps;
-  float* hs = zeros + kSteps + p.wave * (8 + 4 * (kPer - 1)) * Se;
-  float *as = hs + 4 * Se, *mid = as + 4 * Se;  // mid: states after lane 7
-  const int held = p.left < 4 ? p.left : 4;     // channels that exist
-  for (int e = lane; e < 4 * Se; e += 64) {
+  float* hs = zeros + kSteps + p.wave * (1 + kPer) * RW * Se;
+  float *as = hs + RW * Se, *mid = as + RW * Se;  // mid: states at the checkpoints inside a pass
+  for (int e = lane; e < RW * Se; e += 64) {
     const int r = e / Se, s = e - r * Se;
     float A2 = 0.f, h = 0.f;
     if (r < held && s < S) {
-      const int64_t at0 = int64_t(r) * S + s;
-      A2 = kLog2e * a.A[state_at(a, p, 0) + at0];
+      const int64_t at = state_at(a, p, 0) + int64_t(r) * S + s;
+      A2 = kLog2e * a.A[at];
       if (!ENDS) {
-        if (a.initial) h = a.initial[state_at(a, p, p.n) + at0];
-        for (int k = 0; k < p.seg; ++k) {
-          const int64_t at = int64_t(p.n) * a.segs + k;
-          h = __builtin_fmaf(exp2_fast(A2 * a.end_dt[at * a.D + p.d0 + r]), h, a.ends[state_at(a, p, at) + at0]);
-        }
+        if (a.initial) h = a.initial[int64_t(p.n) * a.D * S + at];
+        if (p.seg) h = through(a, p.n, 0, p.seg, 1, at, p.d0 + r, A2, h);
       }
     }
     as[e] = A2;
@@ -218,10 +241,7 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
   for (int e = threadIdx.x; e < kSteps; e += blockDim.x) zeros[e] = 0.f;
   // entry e of [channel][S] in memory, from an array of [channel][Se]
   auto put = [&](float* to, const float* from) {
-    for (int e = lane; e < held * S; e += 64) {
-      const int r = e / S;
-      to[e] = from[e + r * (Se - S)];
-    }
+    for (int e = lane; e < held * S; e += 64) to[e] = from[e + e / S * (Se - S)];
   };
   const T* up = a.u + p.n * a.u_n + p.d * a.u_d + tl * TS;
   const T* dp = a.delta + p.n * a.delta_n + p.d * a.delta_d + tl * TS;
@@ -231,7 +251,7 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
   const float skip = a.Dskip ? a.Dskip[p.d] : 0.f, bias = a.bias ? a.bias[p.d] : 0.f;
   T* op = ENDS ? nullptr : a.out + (int64_t(p.n) * a.D + p.d) * a.L + tl * TS;
   float total = 0.f;
-  Stage<T, TS, NB> st;
+  Stage<T, LN, TS, NB> st;
   Raw8<T> ru[TS / 8] = {}, rd[TS / 8] = {}, rz[TS / 8] = {};
   auto fetch = [&](const T* from, int t0, Raw8<T>* r) {
 #pragma unroll
@@ -271,8 +291,8 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
       const bool two = s + 1 < S;
       const float *b0 = cur + s * kSteps, *b1 = two ? b0 + kSteps : zeros;
       float w[2][TS], b[2][TS], A2[2], in[2], H[2], P[2];
-      lds_steps<TS>(b0, tl, b[0]);
-      lds_steps<TS>(b1, tl, b[1]);
+      lds_steps<LN, TS>(b0, tl, b[0]);
+      lds_steps<LN, TS>(b1, tl, b[1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         A2[i] = as[row * Se + s + i];
@@ -291,31 +311,32 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) H[i] = __builtin_fmaf(P[i], tl == 0 ? in[i] : 0.f, H[i]);
-      scan_row(H[0], H[1], P[0], P[1], in[0], in[1]);
+      scan_lanes<LN>(H, P, in);
       if (ENDS) {
+        if (tl == LN - 1) hs[row * Se + s] = H[0], hs[row * Se + s + 1] = H[1];
+        continue;
+      }
+      float c[2][TS];
+      lds_steps<LN, TS>(b0 + S * kSteps, tl, c[0]);
+      lds_steps<LN, TS>(two ? b0 + (S + 1) * kSteps : zeros, tl, c[1]);
 #pragma unroll
-        for (int j = 0; j < TS; ++j)
+      for (int j = 0; j < TS; ++j) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) in[i] = __builtin_fmaf(w[i][j], in[i], b[i][j]);
-      } else {
-        float c[2][TS];
-        lds_steps<TS>(b0 + S * kSteps, tl, c[0]);
-        lds_steps<TS>(two ? b0 + (S + 1) * kSteps : zeros, tl, c[1]);
-#pragma unroll
-        for (int j = 0; j < TS; ++j) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            in[i] = __builtin_fmaf(w[i][j], in[i], b[i][j]);
-            y[j] = __builtin_fmaf(in[i], c[i][j], y[j]);
-          }
+        for (int i = 0; i < 2; ++i) {
+          in[i] = __builtin_fmaf(w[i][j], in[i], b[i][j]);
+          y[j] = __builtin_fmaf(in[i], c[i][j], y[j]);
         }
       }
-      if (kPer > 1 && !ENDS && tl == 7) mid[row * Se + s] = in[0], mid[row * Se + s + 1] = in[1];
-      if (tl == 15) hs[row * Se + s] = in[0], hs[row * Se + s + 1] = in[1];
+      if (tl % kLanes == kLanes - 1) {
+        float* to = (tl == LN - 1 ? hs : mid + tl / kLanes * RW * Se) + row * Se + s;
+        to[0] = in[0], to[1] = in[1];
+      }
     }
     total += sum;
-    if (kPer > 1 && !ENDS && a.checkpoints && t0 + kChunk < end)
-      put(a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + t0 / kChunk + 1), mid);
+    if (kPer > 1 && a.checkpoints) {
+      for (int k = 1; k < kPer && t0 + k * kChunk < end; ++k)
+        put(a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + t0 / kChunk + k), mid + (k - 1) * RW * Se);
+    }
     if (!ENDS && p.ok) {
 #pragma unroll
       for (int k = 0; k < TS / 8; ++k) {
@@ -340,8 +361,8 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
   if (ENDS) {
     const int64_t at = int64_t(p.n) * a.segs + p.seg;
     put(a.ends + state_at(a, p, at), hs);
-    total = row_sum(total);
-    if (tl == 15 && p.ok) a.end_dt[at * a.D + p.d] = total;
+    for (int m = 1; m < LN; m <<= 1) total += __shfl_xor(total, m);
+    if (tl == 0 && p.ok) a.end_dt[at * a.D + p.d] = total;
     return;
   }
   if (a.final_state && p.seg == a.segs - 1) put(a.final_state + state_at(a, p, p.n), hs);
@@ -390,7 +411,7 @@ __device__ __forceinline__ f32x4 sum_rows(const float* lo, const float* hi) {
 template <typename T, int NB, bool GATE, bool ENDS>
 __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
   extern __shared__ float lds[];
-  const Place p = place(a);
+  const Place p = place<4>(a);
   const int S = a.S, Se = (S + 1) & ~1, rows = ENDS ? S : 2 * S, lane = p.lane, row = p.row, tl = p.tl;
   const int nw = blockDim.x >> 6, batch = a.batch;
   const int len = seq_len(a.lengths, p.n, a.L);
@@ -401,19 +422,16 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
   float* ex = zeros + kChunk;          // [batch][waves][256]
   float* as = ex + (ENDS ? 0 : batch * nw * 256) + p.wave * (ENDS ? 8 : 16) * Se;
   float *rs = as + 4 * Se, *hs = rs + 4 * Se, *dAs = hs + 4 * Se;  // (ENDS: the first two)
-  const int held = p.left < 4 ? p.left : 4;
+  const int held = p.held;
   for (int e = lane; e < 4 * Se; e += 64) {
     const int r0 = e / Se, s = e - r0 * Se;
     float A2 = 0.f, r = 0.f;
     if (r0 < held && s < S) {
-      const int64_t at0 = int64_t(r0) * S + s;
-      A2 = kLog2e * a.A[state_at(a, p, 0) + at0];
+      const int64_t at = state_at(a, p, 0) + int64_t(r0) * S + s;
+      A2 = kLog2e * a.A[at];
       if (!ENDS) {
-        if (a.dfinal) r = a.dfinal[state_at(a, p, p.n) + at0];
-        for (int k = a.segs - 1; k > p.seg; --k) {
-          const int64_t at = int64_t(p.n) * a.segs + k;
-          r = __builtin_fmaf(exp2_fast(A2 * a.end_dt[at * a.D + p.d0 + r0]), r, a.ends[state_at(a, p, at) + at0]);
-        }
+        if (a.dfinal) r = a.dfinal[int64_t(p.n) * a.D * S + at];
+        if (p.seg < a.segs - 1) r = through(a, p.n, a.segs - 1, p.seg, -1, at, p.d0 + r0, A2, r);
       }
     }
     as[e] = A2;
@@ -432,7 +450,7 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
   // (the steps of a row without a channel are all behind its end: they add nothing)
   const int row_len = p.ok ? len - tl * 8 : 0;
   float total = 0.f, dD = 0.f, dbias = 0.f;
-  Stage<T, 8, NB> st;
+  Stage<T, 16, 8, NB> st;
   Raw8<T> ru = {}, rd = {}, rz = {}, rg = {};
   float ck[4];  // the chunk's checkpoint: entries lane, lane + 64, ... of [channel][S]
   auto fetch = [&](int c) {
@@ -496,8 +514,8 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
       const float* b0 = bc + s * kChunk;
       const float* q0 = ENDS ? b0 : b0 + S * kChunk;
       float b[2][8], cc[2][8], w[2][8], A2[2], rin[2], R[2] = {0.f, 0.f}, P[2];
-      lds_steps<8>(q0, tl, cc[0]);
-      lds_steps<8>(two ? q0 + kChunk : zeros, tl, cc[1]);
+      lds_steps<16, 8>(q0, tl, cc[0]);
+      lds_steps<16, 8>(two ? q0 + kChunk : zeros, tl, cc[1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         A2[i] = as[row * Se + s + i];
@@ -514,19 +532,15 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) R[i] = __builtin_fmaf(P[i], tl == 15 ? rin[i] : 0.f, R[i]);
-      scan_row_back(R[0], R[1], P[0], P[1], rin[0], rin[1]);
+      scan_lanes_back(R, P, rin);
       if (ENDS) {
-#pragma unroll
-        for (int j = 7; j >= 0; --j)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) rin[i] = w[i][j] * __builtin_fmaf(dy[j], cc[i][j], rin[i]);
-        if (tl == 0) rs[row * Se + s] = rin[0], rs[row * Se + s + 1] = rin[1];
+        if (tl == 0) rs[row * Se + s] = R[0], rs[row * Se + s + 1] = R[1];
         continue;
       }
       float* exb = ex + (s & (batch - 1)) * nw * 256 + p.wave * 256 + lane * 4;
       float h[2][8], hin[2], H[2] = {0.f, 0.f}, dA[2] = {0.f, 0.f};
-      lds_steps<8>(b0, tl, b[0]);
-      lds_steps<8>(two ? b0 + kChunk : zeros, tl, b[1]);
+      lds_steps<16, 8>(b0, tl, b[0]);
+      lds_steps<16, 8>(two ? b0 + kChunk : zeros, tl, b[1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) hin[i] = hs[row * Se + s + i];
 #pragma unroll
@@ -542,7 +556,7 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
         P[i] = exp2_fast(sum * A2[i]);
         H[i] = __builtin_fmaf(P[i], tl == 0 ? hin[i] : 0.f, H[i]);
       }
-      scan_row(H[0], H[1], P[0], P[1], hin[0], hin[1]);
+      scan_lanes<16>(H, P, hin);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
 #pragma unroll
@@ -763,26 +777,35 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
 }
 
 struct Shape {
-  int per, waves, blks, segs, seg_chunks, chunks;
-  int steps;  // a lane's in a pass (backward: 8)
+  int per, rows, waves, blks, segs, seg_chunks, chunks;  // rows: channels of a wave
+  int steps;  // a lane's in a pass
   int64_t wgs;
 };
 Shape shape_of(const seq_scan_t& p, bool bwd) {
   Shape s = {};
   s.per = p.D / p.G;
-  s.waves = s.per > 16 ? 8 : 4;
-  s.blks = int(ceil_div(s.per, s.waves * 4));
   s.chunks = int(ceil_div(p.L, kChunk));
-  s.steps = !bwd && p.L > 512 && p.S <= 32 ? 16 : 8;
-  const int per = s.steps / 8;  // chunks a pass
-  const int64_t wgs = int64_t(p.N) * p.G * s.blks, waves = wgs * s.waves;
-  int64_t segs = 1;
-  if (waves <= (bwd ? 1024 : 512)) segs = ceil_div(2048, waves);
-  if (segs > s.chunks / (2 * per)) segs = s.chunks / (2 * per);
-  if (segs < 1) segs = 1;
-  s.seg_chunks = int(ceil_div(ceil_div(s.chunks, segs), per) * per);
+  const int64_t waves4 = int64_t(p.N) * p.G * ceil_div(s.per, 4);
+  int64_t want = 1;  // segments
+  if (bwd) {
+    s.rows = 4, s.steps = 8, s.waves = s.per > 16 ? 8 : 4;
+    if (waves4 <= 1024) want = ceil_div(2048, waves4);
+  } else {
+    // (a pass of a whole wave's, 512 steps, fits in LDS for up to 16 states)
+    s.rows = waves4 <= 1024 && p.L > 256 && p.L <= 2048 && p.S <= 16 ? 1 : 4;
+    s.steps = 8, s.waves = p.S > 32 ? 8 : 4;
+    const int64_t waves = s.rows == 1 ? int64_t(p.N) * p.D : waves4;
+    if (waves <= 512) want = ceil_div(2048, waves);
+    // 16 steps are a sixth less work a step, but a pass may waste twice as many
+    if (s.rows == 4 && p.S <= 16 && ceil_div(p.L, 256) * 12 <= ceil_div(p.L, 128) * 7 && want * 256 <= p.L) s.steps = 16;
+  }
+  s.blks = int(ceil_div(s.per, s.waves * s.rows));
+  const int per = 64 / s.rows * s.steps / kChunk;  // chunks a pass
+  const int64_t passes = ceil_div(s.chunks, per);
+  if (want > passes) want = passes;
+  s.seg_chunks = int(ceil_div(passes, want)) * per;
   s.segs = int(ceil_div(s.chunks, s.seg_chunks));
-  s.wgs = wgs * s.segs;
+  s.wgs = int64_t(p.N) * p.G * s.blks * s.segs;
   return s;
 }
 int64_t pad4(int64_t n) { return (n + 3) / 4 * 4; }
@@ -819,21 +842,28 @@ int launch(K kernel, int64_t wgs, int threads, int64_t lds, hipStream_t s, const
 }
 // Staging loads of 16 bytes (fp32: 32) a thread holds for the next pass.
 template <typename F>
-int with_loads(int rows, int steps, int waves, F f) {
-  const int64_t nb = ceil_div(rows * steps * 2, waves * 64);
+int with_loads(int rows, int pass, int waves, F f) {
+  const int64_t nb = ceil_div(rows * pass / 8, waves * 64);
   if (nb <= 1) return f(std::integral_constant<int, 1>{});
   if (nb <= 2) return f(std::integral_constant<int, 2>{});
   if (nb <= 4) return f(std::integral_constant<int, 4>{});
   return f(std::integral_constant<int, 8>{});
 }
 
-template <typename T, int TS, bool ENDS>
-int fwd_pass(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
+template <typename T, int RW, int TS, bool ENDS>
+int fwd_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st) {
+  a.run_segs = ENDS ? s.segs - 1 : s.segs;  // (nothing comes after the last one's end)
+  constexpr int pass = 64 / RW * TS, per = ENDS ? 1 : pass / kChunk;
   const int rows = ENDS ? p.S : 2 * p.S;
-  const int64_t lds = ((2 * rows + 1) * int64_t(16 * TS) + s.waves * (6 + TS / 4) * ((p.S + 1) & ~1)) * 4;
-  return with_loads(rows, TS, s.waves, [&](auto nb) {
-    return launch(scan_fwd_kernel<T, TS, decltype(nb)::value, ENDS>, s.wgs, s.waves * 64, lds, st, a);
+  const int64_t lds = ((2 * rows + 1) * int64_t(pass) + s.waves * (1 + per) * RW * ((p.S + 1) & ~1)) * 4;
+  return with_loads(rows, pass, s.waves, [&](auto nb) {
+    return launch(scan_fwd_kernel<T, RW, TS, decltype(nb)::value, ENDS>, s.wgs / s.segs * a.run_segs, s.waves * 64, lds, st, a);
   });
+}
+template <typename T, bool ENDS>
+int fwd_kind(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
+  if (s.rows == 1) return fwd_pass<T, 1, 8, ENDS>(p, s, a, st);
+  return s.steps == 16 ? fwd_pass<T, 4, 16, ENDS>(p, s, a, st) : fwd_pass<T, 4, 8, ENDS>(p, s, a, st);
 }
 template <typename T>
 int fwd(const seq_scan_t& p, hipStream_t st) {
@@ -845,21 +875,22 @@ int fwd(const seq_scan_t& p, hipStream_t st) {
   a.ends = static_cast<float*>(p.workspace);
   a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * p.D * p.S);
   if (s.segs > 1) {
-    const int rc = s.steps == 16 ? fwd_pass<T, 16, true>(p, s, a, st) : fwd_pass<T, 8, true>(p, s, a, st);
+    const int rc = fwd_kind<T, true>(p, s, a, st);
     if (rc != CONV_OK) return rc;
   }
-  return s.steps == 16 ? fwd_pass<T, 16, false>(p, s, a, st) : fwd_pass<T, 8, false>(p, s, a, st);
+  return fwd_kind<T, false>(p, s, a, st);
 }
 
 // As many as LDS holds beside what S states need: an exchange is two barriers.
 int batch_of(int S) { return S > 32 ? 4 : S > 16 ? 8 : 16; }
 template <typename T, bool GATE, bool ENDS>
-int bwd_pass(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
+int bwd_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st) {
+  a.run_segs = ENDS ? s.segs - 1 : s.segs, a.run_first = ENDS ? 1 : 0;
   const int rows = ENDS ? p.S : 2 * p.S, Se = (p.S + 1) & ~1;
   const int64_t lds =
       ((rows + 1) * int64_t(kChunk) + (ENDS ? 0 : a.batch * s.waves * 256) + s.waves * (ENDS ? 8 : 16) * Se) * 4;
-  return with_loads(rows, 8, s.waves, [&](auto nb) {
-    return launch(scan_bwd_kernel<T, decltype(nb)::value, GATE, ENDS>, s.wgs, s.waves * 64, lds, st, a);
+  return with_loads(rows, kChunk, s.waves, [&](auto nb) {
+    return launch(scan_bwd_kernel<T, decltype(nb)::value, GATE, ENDS>, s.wgs / s.segs * a.run_segs, s.waves * 64, lds, st, a);
   });
 }
 template <typename T, bool GATE>
