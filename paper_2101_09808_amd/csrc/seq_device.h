@@ -141,8 +141,13 @@ __device__ __forceinline__ float softplus(float x) {
   p = __builtin_fmaf(p, q, 0.40024596f);
   p = __builtin_fmaf(p, q, 0.6666632f);
   p = __builtin_fmaf(p, q, 2.f);
-  return __builtin_fmaf(s, p, __builtin_fmaxf(x, 0.f));
+  // (the median of x, 0 and infinity: the larger of x and 0 as one instruction;
+  // a NaN comes through s)
+  return __builtin_fmaf(s, p, __builtin_amdgcn_fmed3f(x, 0.f, __builtin_inff()));
 }
+
+// Keeps what follows in a branch of its own.
+__device__ __forceinline__ void branch() { asm volatile(""); }
 
 // DPP moves within a row of 16 lanes or the wave.  `old` is what lanes without
 // a source keep.

@@ -191,6 +191,7 @@ __device__ __forceinline__ float steps(const Raw8<T>* raw, float bias, bool soft
     for (int j = 0; j < TS; ++j) dt[j] = softplus(dt[j]);
   }
   if (!full) {
+    branch();
 #pragma unroll
     for (int j = 0; j < TS; ++j) dt[j] = j < valid ? dt[j] : 0.f;
   }
@@ -348,6 +349,7 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
           for (int j = 0; j < 8; ++j) yk[j] *= z[j] * sigmoid(z[j]);
         }
         if (!full) {
+          branch();
 #pragma unroll
           for (int j = 0; j < 8; ++j) yk[j] = 8 * k + j < valid ? yk[j] : 0.f;
         }
@@ -473,11 +475,28 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
   int ck_at[4];  // where they belong in [channel][Se]
 #pragma unroll
   for (int k = 0; k < 4; ++k) ck_at[k] = lane + k * 64 + (lane + k * 64) / S * (Se - S);
+  // dB and dC of the batch of states from s0 on, over the waves
+  auto sum_batch = [&](int s0, int c) {
+    float* to = a.part_bc + ((int64_t(p.n) * a.G + p.g) * a.blks + p.blk) * S * 2 * a.chunks * kChunk;
+    for (int o = threadIdx.x; o < batch * 64; o += blockDim.x) {
+      const int i = o >> 6, q = (o & 63) * 4;
+      if (s0 + i < S) {
+        const float* from = ex + i * nw * 256 + q;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < nw; w += 4, from += 1024)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v += *reinterpret_cast<const f32x4*>(from + k * 256);
+        *reinterpret_cast<f32x4*>(to + ((int64_t(s0 + i) * 2 + (q >> 7)) * a.chunks + c) * kChunk + (q & 127)) = v;
+      }
+    }
+  };
+  const int last = (S - 1) & -batch;  // the last batch: summed when the next chunk begins
   if (c0 < cend) fetch(cend - 1);
   for (int c = cend - 1; c >= c0; --c) {
     const int t0 = c * kChunk, valid = row_len - t0;
     const bool full = t0 + kChunk <= len;
-    __syncthreads();  // (the chunk before has been read)
+    __syncthreads();  // (the chunk before has been read, its last batch written)
+    if (!ENDS && c + 1 < cend) sum_batch(last, c + 1);
     st.store(bc, rows);
     if (!ENDS) {
 #pragma unroll
@@ -513,14 +532,14 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
       const bool two = s + 1 < S;
       const float* b0 = bc + s * kChunk;
       const float* q0 = ENDS ? b0 : b0 + S * kChunk;
-      float b[2][8], cc[2][8], w[2][8], A2[2], rin[2], R[2] = {0.f, 0.f}, P[2];
+      float b[2][8], cc[2][8], w[2][8], A2[2], rin[2], R[2] = {0.f, 0.f}, P[2], Q[2];
       lds_steps<16, 8>(q0, tl, cc[0]);
       lds_steps<16, 8>(two ? q0 + kChunk : zeros, tl, cc[1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         A2[i] = as[row * Se + s + i];
         rin[i] = rs[row * Se + s + i];
-        P[i] = exp2_fast(sum * A2[i]);
+        P[i] = Q[i] = exp2_fast(sum * A2[i]);
       }
 #pragma unroll
       for (int j = 7; j >= 0; --j) {
@@ -552,11 +571,8 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
         }
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        P[i] = exp2_fast(sum * A2[i]);
-        H[i] = __builtin_fmaf(P[i], tl == 0 ? hin[i] : 0.f, H[i]);
-      }
-      scan_lanes<16>(H, P, hin);
+      for (int i = 0; i < 2; ++i) H[i] = __builtin_fmaf(Q[i], tl == 0 ? hin[i] : 0.f, H[i]);
+      scan_lanes<16>(H, Q, hin);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
 #pragma unroll
@@ -587,19 +603,11 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
       }
       if (tl == 15) dAs[row * Se + s] += dA[0], dAs[row * Se + s + 1] += dA[1];
       if (tl == 0) rs[row * Se + s] = rin[0], rs[row * Se + s + 1] = rin[1];
-      if ((s + 2 & (batch - 1)) && s + 2 < S) continue;
-      const int s0 = s & -batch;
-      __syncthreads();
-      float* to = a.part_bc + ((int64_t(p.n) * a.G + p.g) * a.blks + p.blk) * S * 2 * a.chunks * kChunk;
-      for (int o = threadIdx.x; o < batch * 128; o += blockDim.x) {
-        const int i = o >> 7, q = (o & 127) * 2;
-        if (s0 + i < S) {
-          f32x2 v = {0.f, 0.f};
-          for (int w2 = 0; w2 < nw; ++w2) v += *reinterpret_cast<const f32x2*>(ex + (i * nw + w2) * 256 + q);
-          *reinterpret_cast<f32x2*>(to + ((int64_t(s0 + i) * 2 + (q >> 7)) * a.chunks + c) * kChunk + (q & 127)) = v;
-        }
+      if ((s + 2 & (batch - 1)) == 0 && s + 2 < S) {
+        __syncthreads();
+        sum_batch(s & -batch, c);
+        __syncthreads();  // (the next batch overwrites it)
       }
-      if (s + 2 < S) __syncthreads();  // (the next batch overwrites these)
     }
     total += sum;
     if (ENDS) continue;
@@ -625,6 +633,7 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
         }
       }
       if (!full) {
+        branch();
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           if (j >= valid) o[j] = od[j] = oz[j] = 0.f;
@@ -639,6 +648,10 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
       store8(a.ddelta + at_row + t0, room, od);
       if (GATE) store8(a.dz + at_row + t0, room, oz);
     }
+  }
+  if (!ENDS && c0 < cend) {
+    __syncthreads();
+    sum_batch(last, c0);
   }
   const int64_t at = int64_t(p.n) * a.segs + p.seg;
   const auto put = [&](float* to, const float* from) {
