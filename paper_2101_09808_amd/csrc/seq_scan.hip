@@ -699,6 +699,7 @@ __global__ __launch_bounds__(256) void scan_sum_kernel(const ScanArgs<T> a, uint
     if (c * kChunk < len) {
       const int64_t step = int64_t(a.S) * 2 * a.chunks * kChunk;
       const float* from = a.part_bc + ng * a.blks * step + (int64_t(s) * 2 + which) * a.chunks * kChunk + int64_t(q) * 4;
+#pragma unroll 16
       for (int b = 0; b < a.blks; ++b) v += *reinterpret_cast<const f32x4*>(from + b * step);
     }
     T* to = (which ? a.dC : a.dB) + ngs * a.L + t;
@@ -711,11 +712,13 @@ __global__ __launch_bounds__(256) void scan_sum_kernel(const ScanArgs<T> a, uint
   const int parts = a.N * a.segs;
   if (i < states) {
     float v = 0.f;
+#pragma unroll 8
     for (int k = 0; k < parts; ++k) v += a.part_A[k * states + i];
     a.dA[i] = v;
   } else if (i < states + int64_t(a.D) * 2) {
     const int64_t e = i - states;
     float v = 0.f;
+#pragma unroll 8
     for (int k = 0; k < parts; ++k) v += a.part_D[k * int64_t(a.D) * 2 + e];
     float* to = e & 1 ? a.dbias : a.dD;
     if (to) to[e >> 1] = v;
@@ -849,26 +852,30 @@ Shape shape_of(const seq_scan_t& p, bool bwd) {
   s.per = p.D / p.G;
   s.chunks = int(ceil_div(p.L, kChunk));
   const int64_t waves4 = int64_t(p.N) * p.G * ceil_div(s.per, 4);
-  int64_t want = 1;  // segments
+  s.rows = 4, s.steps = 8;
   if (bwd) {
-    s.rows = 4, s.steps = 8, s.waves = s.per > 16 ? 8 : 4;
-    if (waves4 <= 1024) want = ceil_div(2048, waves4);
+    s.waves = s.per > 16 ? 8 : 4;
   } else {
-    // (a pass of a whole wave's, 512 steps, fits in LDS for up to 16 states)
-    s.rows = waves4 <= 1024 && p.L > 256 && p.L <= 2048 && p.S <= 16 ? 1 : 4;
-    s.steps = 8, s.waves = p.S > 32 ? 8 : 4;
-    const int64_t waves = s.rows == 1 ? int64_t(p.N) * p.D : waves4;
-    if (waves <= 512) want = ceil_div(2048, waves);
-    // 16 steps are a sixth less work a step, but a pass may waste twice as many
-    if (s.rows == 4 && p.S <= 16 && ceil_div(p.L, 256) * 12 <= ceil_div(p.L, 128) * 7 && want * 256 <= p.L) s.steps = 16;
+    // Few and short rows: a channel has a whole wave, 512 steps a pass (which
+    // fits in LDS for up to 16 states).  2 x 520 x 1001: 15 us, against 22 in
+    // segments; 1 x 1024 x 16384: 176 us, against 148.
+    if (waves4 <= 1024 && p.L > 256 && p.L <= 2048 && p.S <= 16) s.rows = 1;
+    s.waves = p.S > 32 ? 8 : 4;
   }
   s.blks = int(ceil_div(s.per, s.waves * s.rows));
+  // Segments where the chip is less than half full: as many as its 2048 places
+  // for waves (two a SIMD) take at once.
+  const int64_t wgs = int64_t(p.N) * p.G * s.blks, places = 2048 / s.waves;
+  int64_t want = wgs * s.waves <= (bwd || s.rows == 1 ? 1024 : 512) ? places / wgs : 1;
+  // 16 steps a lane are a sixth less work a step, but a pass may waste twice as many.
+  if (!bwd && s.rows == 4 && p.S <= 16 && ceil_div(p.L, 256) * 12 <= ceil_div(p.L, 128) * 7 && want * 256 <= p.L)
+    s.steps = 16;
   const int per = 64 / s.rows * s.steps / kChunk;  // chunks a pass
   const int64_t passes = ceil_div(s.chunks, per);
   if (want > passes) want = passes;
   s.seg_chunks = int(ceil_div(passes, want)) * per;
   s.segs = int(ceil_div(s.chunks, s.seg_chunks));
-  s.wgs = int64_t(p.N) * p.G * s.blks * s.segs;
+  s.wgs = wgs * s.segs;
   return s;
 }
 int64_t pad4(int64_t n) { return (n + 3) / 4 * 4; }
@@ -945,7 +952,7 @@ int fwd(const seq_scan_t& p, hipStream_t st) {
 }
 
 // As many as LDS holds beside what S states need: an exchange is two barriers.
-int batch_of(int S) { return S > 32 ? 4 : S > 16 ? 8 : 16; }
+int batch_of(int S) { return S > 32 ? 4 : S > 16 || S <= 8 ? 8 : 16; }
 template <typename T, bool GATE, bool ENDS>
 int bwd_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st) {
   a.run_segs = ENDS ? s.segs - 1 : s.segs, a.run_first = ENDS ? 1 : 0;
