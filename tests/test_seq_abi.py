@@ -1,0 +1,214 @@
+"""The sequence operators' C ABI (include/seq_ops.h) and Python checks that need
+no GPU: exported symbols, struct layouts, and refusals, which come before
+anything is launched (the pointers here are never followed)."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+import torch
+
+from paper_2101_09808_amd import conv as B
+from paper_2101_09808_amd import seq
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "seq_ops.h")
+FAKE = 0x1000
+
+
+def header():
+    return re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+
+
+def struct(name):
+    """A ctypes mirror of a struct, from the header's text."""
+    body = re.search(r"typedef struct \{([^{}]*)\} %s;" % name, header()).group(1)
+    kinds = {"int32_t": ctypes.c_int32, "int64_t": ctypes.c_int64, "float": ctypes.c_float}
+    fields = []
+    for decl in body.split(";"):
+        decl = decl.strip()
+        if decl:
+            base, names = re.match(r"(?:const )?(\w+)\s*(.*)", decl, flags=re.S).groups()
+            for n in names.split(","):
+                n = n.strip()
+                fields.append((n.strip("* "), ctypes.c_void_p if n.startswith("*") else kinds[base]))
+    return type(name, (ctypes.Structure,), {"_fields_": fields})
+
+
+Conv, Scan, Norm = struct("seq_conv_t"), struct("seq_scan_t"), struct("seq_norm_t")
+
+
+def call(fn, p, size=False):
+    f = getattr(B.lib(), fn)
+    f.restype = ctypes.c_int64 if size else ctypes.c_int
+    f.argtypes = [ctypes.c_void_p] * (1 if size else 2)
+    return f(None if p is None else ctypes.addressof(p), *(() if size else (None,)))
+
+
+def conv(**kw):
+    return Conv(**{**dict(N=2, D=8, L=16, R=4, x=FAKE, weight=FAKE, out=FAKE, dout=FAKE, dx=FAKE, dweight=FAKE), **kw})
+
+
+def scan(**kw):
+    ptrs = {k: FAKE for k in "u delta A B C out checkpoints dout du ddelta dA dB dC".split()}
+    return Scan(**{**dict(N=2, D=8, L=16, S=4, G=2, **ptrs), **kw})
+
+
+def norm(**kw):
+    return Norm(**{**dict(N=2, D=8, L=16, eps=1e-6, x=FAKE, weight=FAKE, out=FAKE), **kw})
+
+
+def test_every_declared_symbol_is_exported():
+    fns = re.findall(r"^\s*(?:int|int64_t)\s+(seq_\w+)\s*\(", header(), flags=re.M)
+    assert len(fns) == 14
+    nm = subprocess.run(["nm", "-D", "--defined-only", B.LIB_PATH], capture_output=True, text=True)
+    for f in fns:
+        assert hasattr(B.lib(), f)
+        if nm.returncode == 0:
+            assert re.search(rf"\bT {f}$", nm.stdout, flags=re.M), f
+
+
+EXTENTS = [(dict(N=0), B.CONV_EINVAL), (dict(D=0), B.CONV_EINVAL), (dict(L=-1), B.CONV_EINVAL),
+           (dict(dtype=2), B.CONV_EINVAL), (dict(L=(1 << 30) + 1), B.CONV_ERANGE),
+           (dict(N=1 << 20, D=1 << 11, G=1), B.CONV_ERANGE)]
+
+
+@pytest.mark.parametrize("bad,status", EXTENTS + [
+    (dict(R=0), B.CONV_EINVAL), (dict(R=9), B.CONV_EINVAL), (dict(activation=2), B.CONV_EINVAL)])
+def test_conv_refusals(bad, status):
+    bad = {k: v for k, v in bad.items() if k != "G"}
+    for fn in ("seq_causal_conv_fwd", "seq_causal_conv_bwd", "seq_causal_conv_step"):
+        assert call(fn, conv(**bad)) == status
+    assert call("seq_causal_conv_bwd_workspace", conv(**bad), True) == status
+
+
+@pytest.mark.parametrize("fn,field", [(f, k) for f, ks in {
+    "seq_causal_conv_fwd": "x weight out", "seq_causal_conv_bwd": "x weight dout dx dweight"}.items()
+    for k in ks.split()])
+def test_conv_null_pointers(fn, field):
+    assert call(fn, conv(**{field: None})) == B.CONV_ENULL
+    assert call(fn, None) == B.CONV_ENULL
+
+
+def test_conv_step_refusals():
+    assert call("seq_causal_conv_step", conv()) == B.CONV_EINVAL  # L = 16
+    assert call("seq_causal_conv_step", conv(L=1)) == B.CONV_ENULL  # no states
+    assert call("seq_causal_conv_step", conv(L=1, initial_state=FAKE)) == B.CONV_ENULL
+    assert call("seq_causal_conv_step", conv(L=1, initial_state=FAKE, final_state=FAKE, lengths=FAKE)) == B.CONV_EINVAL
+
+
+def test_conv_work_past_one_launch():
+    big = dict(N=1 << 15, D=1 << 14, L=128)  # 2^33 threads of eight outputs
+    assert call("seq_causal_conv_fwd", conv(**big)) == B.CONV_ERANGE
+
+
+def test_conv_workspace():
+    p = conv(D=8, N=4, L=5000)
+    n = call("seq_causal_conv_bwd_workspace", p, True)
+    assert n > 0
+    assert call("seq_causal_conv_bwd", p) in (B.CONV_ENULL, B.CONV_ESCRATCH)
+    p.workspace, p.workspace_bytes = FAKE, n - 1
+    assert call("seq_causal_conv_bwd", p) == B.CONV_ESCRATCH
+    assert call("seq_causal_conv_bwd_workspace", conv(D=4096), True) == 0
+
+
+@pytest.mark.parametrize("bad,status", EXTENTS + [
+    (dict(S=0), B.CONV_EINVAL), (dict(S=65), B.CONV_EINVAL), (dict(G=0), B.CONV_EINVAL), (dict(G=3), B.CONV_EINVAL),
+    (dict(reserved=1), B.CONV_EINVAL)])
+def test_scan_refusals(bad, status):
+    for fn in ("seq_selective_scan_fwd", "seq_selective_scan_bwd", "seq_selective_scan_step"):
+        assert call(fn, scan(**bad)) == status
+    for fn in ("seq_selective_scan_fwd_workspace", "seq_selective_scan_bwd_workspace"):
+        assert call(fn, scan(**bad), True) == status
+
+
+@pytest.mark.parametrize("fn,field", [(f, k) for f, ks in {
+    "seq_selective_scan_fwd": "u delta A B C out",
+    "seq_selective_scan_bwd": "u delta A B C checkpoints dout du ddelta dA dB dC"}.items() for k in ks.split()])
+def test_scan_null_pointers(fn, field):
+    assert call(fn, scan(**{field: None})) == B.CONV_ENULL
+    assert call(fn, None) == B.CONV_ENULL
+
+
+def test_scan_missing_gradients_and_workspaces():
+    for have in ("z", "Dskip", "delta_bias"):
+        assert call("seq_selective_scan_bwd", scan(**{have: FAKE})) == B.CONV_ENULL
+    p = scan()
+    n = call("seq_selective_scan_bwd_workspace", p, True)
+    assert n > 0
+    assert call("seq_selective_scan_bwd", p) == B.CONV_ENULL
+    p.workspace, p.workspace_bytes = FAKE, n - 1
+    assert call("seq_selective_scan_bwd", p) == B.CONV_ESCRATCH
+    p = scan(D=16, L=1 << 16)  # few rows, long: cut into segments
+    n = call("seq_selective_scan_fwd_workspace", p, True)
+    assert n > 0
+    assert call("seq_selective_scan_fwd", p) == B.CONV_ENULL
+    p.workspace, p.workspace_bytes = FAKE, n - 1
+    assert call("seq_selective_scan_fwd", p) == B.CONV_ESCRATCH
+    assert call("seq_selective_scan_fwd_workspace", scan(N=64, D=4096, L=4096), True) == 0
+
+
+def test_scan_step_refusals():
+    assert call("seq_selective_scan_step", scan(checkpoints=None)) == B.CONV_EINVAL  # L = 16
+    ok = dict(L=1, checkpoints=None)
+    assert call("seq_selective_scan_step", scan(L=1)) == B.CONV_EINVAL  # checkpoints
+    assert call("seq_selective_scan_step", scan(**ok)) == B.CONV_ENULL
+    assert call("seq_selective_scan_step", scan(**ok, initial_state=FAKE)) == B.CONV_ENULL
+    assert call("seq_selective_scan_step", scan(**ok, initial_state=FAKE, lengths=FAKE)) == B.CONV_EINVAL
+
+
+NORMS = ("seq_norm_pre_fwd", "seq_norm_post_fwd", "seq_norm_pre_bwd", "seq_norm_post_bwd")
+
+
+@pytest.mark.parametrize("bad,status", [(b, s) for b, s in EXTENTS if "G" not in b] + [
+    (dict(res_dtype=1), B.CONV_EINVAL),  # fp32 with a bf16 residual
+    (dict(eps=-1.0), B.CONV_EINVAL), (dict(eps=float("nan")), B.CONV_EINVAL)])
+def test_norm_refusals(bad, status):
+    for fn in NORMS:
+        assert call(fn, norm(**bad)) == status
+    assert call("seq_norm_bwd_workspace", norm(**bad), True) == status
+
+
+def test_norm_combinations():
+    for fn in ("seq_norm_pre_fwd", "seq_norm_post_fwd"):
+        for k in ("x", "weight", "out"):
+            assert call(fn, norm(**{k: None})) == B.CONV_ENULL
+    assert call("seq_norm_pre_fwd", norm(gate=FAKE)) == B.CONV_EINVAL
+    assert call("seq_norm_post_fwd", norm(sum=FAKE)) == B.CONV_EINVAL
+    pre = dict(sum=FAKE, dout=FAKE, dx=FAKE, dweight=FAKE)
+    for k in pre:
+        assert call("seq_norm_pre_bwd", norm(**{**pre, k: None})) == B.CONV_ENULL
+    assert call("seq_norm_pre_bwd", norm(**pre, scale=FAKE)) == B.CONV_ENULL  # no dscale
+    assert call("seq_norm_pre_bwd", norm(**pre, gate=FAKE)) == B.CONV_EINVAL
+    post = dict(dout=FAKE, dx=FAKE, dweight=FAKE)
+    for k in post:
+        assert call("seq_norm_post_bwd", norm(**{**post, k: None})) == B.CONV_ENULL
+    assert call("seq_norm_post_bwd", norm(**post, gate=FAKE)) == B.CONV_ENULL  # no dgate
+    assert call("seq_norm_post_bwd", norm(**post, dsum=FAKE)) == B.CONV_EINVAL
+    for fn, kw in (("seq_norm_pre_bwd", pre), ("seq_norm_post_bwd", post)):
+        p = norm(**kw)
+        n = call("seq_norm_bwd_workspace", p, True)
+        assert n > 0 and call(fn, p) == B.CONV_ENULL
+        p.workspace, p.workspace_bytes = FAKE, n - 1
+        assert call(fn, p) == B.CONV_ESCRATCH
+
+
+def test_python_refuses_what_is_not_on_the_gpu():
+    x, w = torch.zeros(2, 3, 4), torch.zeros(3, 4)
+    s, b = torch.zeros(2, 3, 5), torch.zeros(2, 1, 5, 4)
+    calls = [lambda v: seq.causal_conv_fwd(v, w), lambda v: seq.causal_conv_bwd(x, v, w),
+             lambda v: seq.causal_conv_step(v, s, w), lambda v: seq.selective_scan_fwd(v, x, w, b, b),
+             lambda v: seq.selective_scan_bwd(x, v, x, w, b, b, s), lambda v: seq.selective_scan_step(v, s, x, w, b, b),
+             lambda v: seq.norm_pre_fwd(v, w), lambda v: seq.norm_pre_bwd(v, x, w), lambda v: seq.norm_post_fwd(v, w),
+             lambda v: seq.norm_post_bwd(x, v, w)]
+    for f in calls:
+        with pytest.raises(ValueError, match="GPU"):
+            f(x)
+        with pytest.raises(TypeError, match="tensor"):
+            f(None)
+
+
+def test_native_calls_count_their_arguments():
+    with pytest.raises(TypeError, match="arguments"):
+        seq.native().causal_conv_fwd(1)
