@@ -197,7 +197,9 @@ int seq_norm_pre_fwd(const seq_norm_t* p, void* stream);
 int seq_norm_pre_bwd(const seq_norm_t* p, void* stream);
 int seq_norm_post_fwd(const seq_norm_t* p, void* stream);
 int seq_norm_post_bwd(const seq_norm_t* p, void* stream);
-/* Bytes of workspace that either backward call needs, or a negative status. */
+/* Bytes of workspace that either forward (backward) call needs, or a negative
+ * status; they depend on the extents and types alone. */
+int64_t seq_norm_fwd_workspace(const seq_norm_t* p);
 int64_t seq_norm_bwd_workspace(const seq_norm_t* p);
 
 #ifdef __cplusplus

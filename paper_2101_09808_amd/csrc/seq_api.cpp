@@ -119,6 +119,10 @@ int seq_norm_post_bwd(const seq_norm_t* p, void* stream) {
     return CONV_ENULL;
   return launch_norm_bwd(*p, true, stream);
 }
+int64_t seq_norm_fwd_workspace(const seq_norm_t* p) {
+  const int rc = check_norm(p);
+  return rc ? rc : norm_fwd_workspace(*p);
+}
 int64_t seq_norm_bwd_workspace(const seq_norm_t* p) {
   const int rc = check_norm(p);
   return rc ? rc : norm_bwd_workspace(*p);

@@ -24,6 +24,7 @@ int launch_scan_fwd(const seq_scan_t& p, void* stream);
 int launch_scan_bwd(const seq_scan_t& p, void* stream);
 int launch_scan_step(const seq_scan_t& p, void* stream);
 
+int64_t norm_fwd_workspace(const seq_norm_t& p);
 int64_t norm_bwd_workspace(const seq_norm_t& p);
 int launch_norm_fwd(const seq_norm_t& p, bool post, void* stream);
 int launch_norm_bwd(const seq_norm_t& p, bool post, void* stream);

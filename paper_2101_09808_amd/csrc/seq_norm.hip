@@ -43,7 +43,12 @@ struct NormArgs {
   void *dx, *dgate, *dresidual;
   float *partial;  // backward: [workgroups][2][D]
   uint32_t tiles, row_tiles;  // in all, of one n
+  int parts, part;  // of the channels; a part's channels
+  float *stats;     // [tiles][parts][sums]
 };
+
+// What a launch does: everything, a part's sums, or what follows them.
+enum Phase { kWhole, kSums, kRest };
 
 __device__ __forceinline__ float silu(float z) { return z * sigmoid(z); }
 
@@ -88,10 +93,28 @@ struct ColumnSums {
       total[tid] = v;
     }
     __syncthreads();
+    share(s);
+  }
+  __device__ __forceinline__ void share(float (*s)[8]) const {
 #pragma unroll
     for (int k = 0; k < NS; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[k][j] = total[(k * CL + tid % CL) * 8 + j];
+      for (int j = 0; j < 8; ++j) s[k][j] = total[(k * CL + int(threadIdx.x) % CL) * 8 + j];
+  }
+  // The sums of `parts` launched workgroups, from [parts][C]; to it, one's own.
+  __device__ __forceinline__ void take(const float* stats, int parts, float (*s)[8]) {
+    const int tid = threadIdx.x;
+    if (tid < C) {
+      float v = 0.f;
+#pragma unroll 8
+      for (int r = 0; r < parts; ++r) v += stats[r * C + tid];
+      total[tid] = v;
+    }
+    __syncthreads();
+    share(s);
+  }
+  __device__ __forceinline__ void give(float* stats) const {
+    if (threadIdx.x < C) stats[threadIdx.x] = total[threadIdx.x];
   }
 };
 
@@ -120,12 +143,14 @@ __device__ __forceinline__ const void* at_cols(const void* base, int n, int64_t 
   return base ? static_cast<const T*>(base) + n * n_stride + col : nullptr;
 }
 
-template <typename T, typename R, bool POST, int NT, int CL, int H>
+template <typename T, typename R, bool POST, int PHASE, int NT, int CL, int H>
 __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
   using Out = typename NormTypes<T, R, POST>::Out;
   __shared__ ColumnSums<NT, CL, 1> sums;
   constexpr int RS = NT / CL;
-  const uint32_t tile = tile_of(blockIdx.x, a.tiles);
+  const uint32_t part = PHASE ? blockIdx.x % a.parts : 0, tile = PHASE ? blockIdx.x / a.parts : tile_of(blockIdx.x, a.tiles);
+  const int rows = PHASE && int(part + 1) * a.part < a.D ? int(part + 1) * a.part : a.D;  // (the part's end)
+  float* const stats = PHASE ? a.stats + (int64_t(tile) * a.parts + (PHASE == kSums ? part : 0)) * (CL * 8) : nullptr;
   const int n = int(tile / a.row_tiles);
   const int col0 = int(tile - n * a.row_tiles) * (CL * 8), col = col0 + int(threadIdx.x) % CL * 8, nv = a.L - col;
   const void* const xp = at_cols<T>(a.x, n, a.x_n, col);
@@ -136,7 +161,7 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
   auto body = [&](auto inside) {
     constexpr bool IN = decltype(inside)::value;
     float s[1][8] = {};
-    int d0 = threadIdx.x / CL;
+    int d0 = int(threadIdx.x) / CL + (PHASE ? int(part) * a.part : 0);
     // x and gate (before: the residual) of a channel, its r or v
     auto terms = [&](const Raw8<T>& x, const Raw8<T>& g, const Raw8<R>& r, int d, float* v) {
       unpack8(x, v);
@@ -155,6 +180,7 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
       }
     };
     auto first = [&](const float* v, int d) {
+      if (PHASE == kRest) return;
       if (!POST && a.sum) store8(static_cast<R*>(a.sum) + base + int64_t(d) * a.L, IN ? 8 : nv, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[0][j] = __builtin_fmaf(v[j], v[j], s[0][j]);
@@ -177,7 +203,7 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
     Raw8<R> r[H];
 #pragma unroll
     for (int k = 0; k < H; ++k) {
-      const int d = d0 + k * RS, dc = d < a.D ? d : a.D - 1;
+      const int d = d0 + k * RS, dc = d < rows ? d : rows - 1;
       x[k] = cols<IN, T>(xp, dc, a.x_d, nv);
       g[k] = has_g ? cols<IN, T>(gp, dc, a.gate_d, nv) : Raw8<T>{};
       r[k] = has_r ? cols<IN, R>(rp, dc, a.res_d, nv) : Raw8<R>{};
@@ -186,7 +212,7 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
 #pragma unroll
     for (int k = 0; k < H; ++k) {
       const int d = d0 + k * RS;
-      if (d < a.D) {
+      if (d < rows) {
         terms(x[k], g[k], r[k], d, held[k]);
         first(held[k], d);
       }
@@ -196,22 +222,29 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
       rr = has_r ? cols<IN, R>(rp, d, a.res_d, nv) : Raw8<R>{};
       terms(xx, gg, rr, d, v);
     };
-    for (int d = d0 + H * RS; d < a.D; d += RS) {
+    for (int d = d0 + H * RS; PHASE != kRest && d < rows; d += RS) {
       float v[8];
       Raw8<R> rr;
       again_at(d, v, rr);
       first(v, d);
     }
-    sums.run(s);
+    if (PHASE == kRest)
+      sums.take(stats, a.parts, s);
+    else
+      sums.run(s);
+    if (PHASE == kSums) {
+      sums.give(stats);
+      return;
+    }
     d0 = fresh(d0);
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[0][j] = __builtin_amdgcn_rsqf(__builtin_fmaf(s[0][j], a.inv_d, a.eps));
 #pragma unroll
     for (int k = 0; k < H; ++k) {
       const int d = d0 + k * RS;
-      if (d < a.D) second(held[k], r[k], d);
+      if (d < rows) second(held[k], r[k], d);
     }
-    for (int d = d0 + H * RS; d < a.D; d += RS) {
+    for (int d = d0 + H * RS; d < rows; d += RS) {
       float v[8];
       Raw8<R> rr;
       again_at(d, v, rr);
@@ -253,17 +286,21 @@ __device__ __forceinline__ void finish(const Elem& e, float rstd, float m, float
 // channel's parameter gradients over its columns and tiles, in registers for the
 // channels that stay there, the others in its own part of `partial` (always the
 // same thread, so in order); norm_sum_kernel adds the parts.
-template <typename T, typename R, bool POST, int NT, int CL, int H>
+template <typename T, typename R, bool POST, int PHASE, int NT, int CL, int H>
 __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormArgs a) {
   using Out = typename NormTypes<T, R, POST>::Out;
   using V = typename std::conditional<POST, T, R>::type;  // of x (before: of sum)
   __shared__ ColumnSums<NT, CL, 2> sums;
   constexpr int RS = NT / CL;
-  float* pw = a.partial + int64_t(blockIdx.x) * 2 * a.D;
+  const uint32_t part = PHASE ? blockIdx.x % a.parts : 0, wg = PHASE ? blockIdx.x / a.parts : blockIdx.x;
+  const int rows = PHASE && int(part + 1) * a.part < a.D ? int(part + 1) * a.part : a.D;  // (the part's end)
+  const int row0 = PHASE ? int(part) * a.part : 0;
+  float* const stats = PHASE ? a.stats + (int64_t(wg) * a.parts + (PHASE == kSums ? part : 0)) * (CL * 16) : nullptr;
+  float* pw = a.partial + int64_t(wg) * 2 * a.D;
   float* ps = pw + a.D;
   float dws[H] = {}, dscs[H] = {};
-  for (uint32_t b = blockIdx.x; b < a.tiles; b += gridDim.x) {
-    const uint32_t tile = tile_of(b, a.tiles);
+  for (uint32_t b = wg; b < a.tiles; b += PHASE ? a.tiles : gridDim.x) {
+    const uint32_t tile = PHASE ? b : tile_of(b, a.tiles);
     const int n = int(tile / a.row_tiles);
     const int col0 = int(tile - n * a.row_tiles) * (CL * 8), col = col0 + int(threadIdx.x) % CL * 8, nv = a.L - col;
     const int64_t v_d = POST ? a.x_d : a.res_d, base = int64_t(n) * a.D * a.L + col;
@@ -278,7 +315,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormArgs a) {
     auto body = [&](auto inside) {
       constexpr bool IN = decltype(inside)::value;
       float s[2][8] = {};
-      int d0 = fresh(threadIdx.x / CL);
+      int d0 = fresh(threadIdx.x / CL) + row0;
       auto first = [&](const Raw8<V>& vr, const Raw8<T>& zr, const Raw8<Out>& gr, int d) {
         float v[8], z[8], g[8];
         unpack8(vr, v);
@@ -335,7 +372,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormArgs a) {
       auto dsum = [&](int d) { return has_s ? cols<IN, R>(sp, d, a.dsum_d, nv) : Raw8<R>{}; };
 #pragma unroll
       for (int k = 0; k < H; ++k) {
-        const int d = d0 + k * RS, dc = d < a.D ? d : a.D - 1;
+        const int d = d0 + k * RS, dc = d < rows ? d : rows - 1;
         v[k] = cols<IN, V>(vp, dc, v_d, nv);
         g[k] = cols<IN, Out>(dp, dc, a.dout_d, nv);
         z[k] = gate_or_x(dc);
@@ -343,12 +380,19 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormArgs a) {
       }
 #pragma unroll
       for (int k = 0; k < H; ++k) {
-        if (d0 + k * RS < a.D) first(v[k], z[k], g[k], d0 + k * RS);
+        if (PHASE != kRest && d0 + k * RS < rows) first(v[k], z[k], g[k], d0 + k * RS);
         __builtin_amdgcn_sched_barrier(0);
       }
-      for (int d = d0 + H * RS; d < a.D; d += RS)
+      for (int d = d0 + H * RS; PHASE != kRest && d < rows; d += RS)
         first(cols<IN, V>(vp, d, v_d, nv), POST ? gate_or_x(d) : Raw8<T>{}, cols<IN, Out>(dp, d, a.dout_d, nv), d);
-      sums.run(s);
+      if (PHASE == kRest)
+        sums.take(stats, a.parts, s);
+      else
+        sums.run(s);
+      if (PHASE == kSums) {
+        sums.give(stats);
+        return;
+      }
       d0 = fresh(d0);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -358,17 +402,17 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormArgs a) {
       }
 #pragma unroll
       for (int k = 0; k < H; ++k) {
-        if (d0 + k * RS < a.D)
+        if (d0 + k * RS < rows)
           second(again(v[k]), again(z[k]), again(g[k]), ds[k], d0 + k * RS, dws[k], dscs[k]);
         __builtin_amdgcn_sched_barrier(0);  // (one channel's registers at a time)
       }
-      for (int d = d0 + H * RS; d < a.D; d += RS) {
+      for (int d = d0 + H * RS; d < rows; d += RS) {
         float dw = 0.f, dsc = 0.f;
         second(cols<IN, V>(vp, d, v_d, nv), gate_or_x(d), cols<IN, Out>(dp, d, a.dout_d, nv), dsum(d), d, dw, dsc);
 #pragma unroll
         for (int m = 1; m < CL; m <<= 1) dw += __shfl_xor(dw, m), dsc += __shfl_xor(dsc, m);
         if (threadIdx.x % CL == 0) {
-          const bool more = b != blockIdx.x;
+          const bool more = b != wg;
           pw[d] = more ? pw[d] + dw : dw;
           ps[d] = more ? ps[d] + dsc : dsc;
         }
@@ -379,12 +423,13 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormArgs a) {
     else
       body(std::false_type{});
   }
+  if (PHASE == kSums) return;
 #pragma unroll
   for (int k = 0; k < H; ++k) {
-    const int d = threadIdx.x / CL + k * RS;
+    const int d = int(threadIdx.x) / CL + row0 + k * RS;
 #pragma unroll
     for (int m = 1; m < CL; m <<= 1) dws[k] += __shfl_xor(dws[k], m), dscs[k] += __shfl_xor(dscs[k], m);
-    if (threadIdx.x % CL == 0 && d < a.D) pw[d] = dws[k], ps[d] = dscs[k];
+    if (threadIdx.x % CL == 0 && d < rows) pw[d] = dws[k], ps[d] = dscs[k];
   }
 }
 
@@ -392,11 +437,24 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormArgs a) {
 // thread keeps its column: the threads in use are a multiple of L.
 constexpr int kFlatMax = 15;
 
-template <int NT, int NS>
-__device__ __forceinline__ void flat_sums(float* s, int L, int used, float* lds) {
+// PHASE: as for the tiles; `stats` has [parts][NS][L] of the sequence.
+template <int PHASE, int NT, int NS>
+__device__ __forceinline__ void flat_sums(float* s, int L, int used, float* lds, float* stats, int part, int parts) {
   const int tid = threadIdx.x;
-  float* part = lds + NS * NT;      // [NS][16][L]
-  float* total = part + NS * 16 * (kFlatMax + 1);
+  float* some = lds + NS * NT;  // [NS][16][L]
+  float* total = some + NS * 16 * (kFlatMax + 1);
+  if (PHASE == kRest) {
+    if (tid < NS * L) {
+      float v = 0.f;
+#pragma unroll 8
+      for (int r = 0; r < parts; ++r) v += stats[r * NS * L + tid];
+      total[tid] = v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NS; ++k) s[k] = total[k * L + tid % L];
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < NS; ++k) lds[k * NT + tid] = tid < used ? s[k] : 0.f;
   __syncthreads();
@@ -405,7 +463,7 @@ __device__ __forceinline__ void flat_sums(float* s, int L, int used, float* lds)
     for (int k = 0; k < NS; ++k) {
       float v = 0.f;
       for (int i = tid; i < used; i += 16 * L) v += lds[k * NT + i];
-      part[k * 16 * L + tid] = v;
+      some[k * 16 * L + tid] = v;
     }
   }
   __syncthreads();
@@ -413,10 +471,14 @@ __device__ __forceinline__ void flat_sums(float* s, int L, int used, float* lds)
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
       float v = 0.f;
-      for (int i = 0; i < 16; ++i) v += part[k * 16 * L + i * L + tid];
-      total[k * L + tid] = v;
+      for (int i = 0; i < 16; ++i) v += some[k * 16 * L + i * L + tid];
+      if (PHASE == kSums)
+        stats[(part * NS + k) * L + tid] = v;
+      else
+        total[k * L + tid] = v;
     }
   }
+  if (PHASE == kSums) return;
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < NS; ++k) s[k] = total[k * L + tid % L];
@@ -434,24 +496,27 @@ __device__ __forceinline__ float normed1(const NormArgs& a, int n, int d, int l)
   return __builtin_fmaf(a.scale ? a.scale[d] : 1.f, x, r);
 }
 
-template <typename T, typename R, bool POST, int NT>
+template <typename T, typename R, bool POST, int PHASE, int NT>
 __global__ __launch_bounds__(NT) void norm_fwd_flat_kernel(const NormArgs a) {
   using Out = typename NormTypes<T, R, POST>::Out;
   __shared__ float lds[flat_lds<NT, 1>()];
-  const int n = blockIdx.x, tid = threadIdx.x, per = NT / a.L, used = per * a.L, l = tid % a.L, d0 = tid / a.L;
+  const int part = PHASE ? int(blockIdx.x) % a.parts : 0, n = PHASE ? int(blockIdx.x) / a.parts : int(blockIdx.x);
+  const int rows = PHASE && (part + 1) * a.part < a.D ? (part + 1) * a.part : a.D;
+  float* const stats = PHASE ? a.stats + int64_t(n) * a.parts * a.L : nullptr;
+  const int tid = threadIdx.x, per = NT / a.L, used = per * a.L, l = tid % a.L, d0 = tid / a.L + part * a.part;
   const int64_t base = int64_t(n) * a.D * a.L + l;
   float s[1] = {0.f};
-  if (tid < used) {
-    for (int d = d0; d < a.D; d += per) {
+  if (PHASE != kRest && tid < used) {
+    for (int d = d0; d < rows; d += per) {
       const float v = normed1<T, R, POST>(a, n, d, l);
       if (!POST && a.sum) static_cast<R*>(a.sum)[base + int64_t(d) * a.L] = from_f<R>(v);
       s[0] = __builtin_fmaf(v, v, s[0]);
     }
   }
-  flat_sums<NT, 1>(s, a.L, used, lds);
-  if (tid >= used) return;
+  flat_sums<PHASE, NT, 1>(s, a.L, used, lds, stats, part, a.parts);
+  if (PHASE == kSums || tid >= used) return;
   const float rstd = __builtin_amdgcn_rsqf(__builtin_fmaf(s[0], a.inv_d, a.eps));
-  for (int d = d0; d < a.D; d += per) {
+  for (int d = d0; d < rows; d += per) {
     float o = a.weight[d] * (normed1<T, R, POST>(a, n, d, l) * rstd);
     if (POST) {
       const float r = a.residual ? to_f(static_cast<const R*>(a.residual)[n * a.res_n + d * a.res_d + l]) : 0.f;
@@ -462,14 +527,17 @@ __global__ __launch_bounds__(NT) void norm_fwd_flat_kernel(const NormArgs a) {
 }
 
 // (a column has a part of its own in `partial`: [workgroups][L][2][D])
-template <typename T, typename R, bool POST, int NT>
+template <typename T, typename R, bool POST, int PHASE, int NT>
 __global__ __launch_bounds__(NT) void norm_bwd_flat_kernel(const NormArgs a) {
   using Out = typename NormTypes<T, R, POST>::Out;
   __shared__ float lds[flat_lds<NT, 2>()];
-  const int tid = threadIdx.x, per = NT / a.L, used = per * a.L, l = tid % a.L, d0 = tid / a.L;
-  float* pw = a.partial + (int64_t(blockIdx.x) * a.L + l) * 2 * a.D;
+  const int part = PHASE ? int(blockIdx.x) % a.parts : 0, wg = PHASE ? int(blockIdx.x) / a.parts : int(blockIdx.x);
+  const int rows = PHASE && (part + 1) * a.part < a.D ? (part + 1) * a.part : a.D;
+  float* const stats = PHASE ? a.stats + int64_t(wg) * a.parts * 2 * a.L : nullptr;
+  const int tid = threadIdx.x, per = NT / a.L, used = per * a.L, l = tid % a.L, d0 = tid / a.L + part * a.part;
+  float* pw = a.partial + (int64_t(wg) * a.L + l) * 2 * a.D;
   float* ps = pw + a.D;
-  for (int n = blockIdx.x; n < a.N; n += gridDim.x) {
+  for (int n = wg; n < a.N; n += PHASE ? a.N : int(gridDim.x)) {
     const int64_t base = int64_t(n) * a.D * a.L + l;
     auto read = [&](int d) {
       Elem e = {};
@@ -485,18 +553,19 @@ __global__ __launch_bounds__(NT) void norm_bwd_flat_kernel(const NormArgs a) {
       return e;
     };
     float s[2] = {0.f, 0.f};
-    if (tid < used) {
-      for (int d = d0; d < a.D; d += per) {
+    if (PHASE != kRest && tid < used) {
+      for (int d = d0; d < rows; d += per) {
         const Elem e = read(d);
         s[0] = __builtin_fmaf(e.v, e.v, s[0]);
         s[1] = __builtin_fmaf(e.h, e.v, s[1]);
       }
     }
-    flat_sums<NT, 2>(s, a.L, used, lds);
+    flat_sums<PHASE, NT, 2>(s, a.L, used, lds, stats, part, a.parts);
+    if (PHASE == kSums) return;
     if (tid < used) {
       const float rstd = __builtin_amdgcn_rsqf(__builtin_fmaf(s[0], a.inv_d, a.eps));
       const float m = s[1] * rstd * a.inv_d;
-      for (int d = d0; d < a.D; d += per) {
+      for (int d = d0; d < rows; d += per) {
         const Elem e = read(d);
         const int64_t at = base + int64_t(d) * a.L;
         const float ds = !POST && a.dsum ? to_f(static_cast<const R*>(a.dsum)[n * a.dsum_n + d * a.dsum_d + l]) : 0.f;
@@ -506,7 +575,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_flat_kernel(const NormArgs a) {
         if (POST && a.gate) static_cast<T*>(a.dgate)[at] = from_f<T>(dg);
         if (!POST && a.dresidual) static_cast<R*>(a.dresidual)[at] = from_f<R>(dr);
         if (POST) dsc *= a.weight[d];
-        const bool more = n != int(blockIdx.x);
+        const bool more = n != wg;
         pw[d] = more ? pw[d] + dw : dw;
         ps[d] = more ? ps[d] + dsc : dsc;
       }
@@ -537,57 +606,78 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* partial, in
 struct Shape {
   bool flat;
   int nt, cl;
-  int64_t tiles, row_tiles;
-  int wgs;  // backward
+  int64_t tiles, row_tiles;  // (flat: sequences)
+  int parts, part;           // 0: the channels are not cut
+  int wgs;                   // backward: with a part of the parameters' gradients each
 };
+// Channels of a thread that stay in registers (bytes of up to four tensors' eight columns).
+int held(const seq_norm_t& p) { return p.res_dtype == CONV_DTYPE_BF16 ? 4 : 2; }
 Shape shape_of(const seq_norm_t& p) {
   Shape s = {};
   s.flat = p.L <= kFlatMax;
   if (s.flat) {
+    s.tiles = p.N;
     s.nt = int64_t(p.D) * p.L > 2048 ? 1024 : 256;
-    s.wgs = p.N < 512 ? p.N : 512;
-    return s;
+    s.part = 256 / p.L * 8;
+  } else {
+    // Wide tiles use whole cache lines, but every CU should have one, and a
+    // thread's channels should mostly stay in registers.  Forward and backward
+    // with CL = 2, 4, 8: 80 us at 4 for bf16 4 x 2048 x 2048 (256 tiles; 86 at 2,
+    // 100 at 8), 59 us at 2 for fp32 3 x 1000 x 1333 (252 tiles; 80 at 4).
+    s.cl = 8;
+    const auto narrow = [&] { return p.L <= s.cl * 4 || int64_t(p.D) * s.cl > 8192; };
+    while (s.cl > 2 && (narrow() || p.N * ceil_div(p.L, s.cl * 8) < 256)) s.cl /= 2;
+    s.nt = int64_t(p.D) * s.cl > 512 ? 1024 : 256;
+    s.row_tiles = ceil_div(p.L, s.cl * 8);
+    s.tiles = s.row_tiles * p.N;
+    s.part = 256 / s.cl * held(p);
   }
-  // Wide tiles use whole cache lines, but every CU should have one, and a
-  // thread's channels should mostly stay in registers.  Forward and backward
-  // with CL = 2, 4, 8: 80 us at 4 for bf16 4 x 2048 x 2048 (256 tiles; 86 at 2,
-  // 100 at 8), 59 us at 2 for fp32 3 x 1000 x 1333 (252 tiles; 80 at 4).
-  s.cl = 8;
-  while (s.cl > 2 && (p.L <= s.cl * 4 || p.N * ceil_div(p.L, s.cl * 8) < 256 || int64_t(p.D) * s.cl > 8192)) s.cl /= 2;
-  s.nt = int64_t(p.D) * s.cl > 512 ? 1024 : 256;
-  s.row_tiles = ceil_div(p.L, s.cl * 8);
-  s.tiles = s.row_tiles * p.N;
-  s.wgs = int(s.tiles < 256 ? s.tiles : 256);
+  // Cut where under half of the CUs would have work and a part is well below
+  // all channels.  bf16 9 x 2816 x 53, forward and
+  // backward: 110 us whole, 45 cut.
+  if (s.tiles < 128 && p.D >= 2 * s.part) {
+    s.nt = 256;
+    s.parts = int(ceil_div(p.D, s.part));
+  }
+  s.wgs = int(s.parts ? s.tiles : s.flat ? (s.tiles < 512 ? s.tiles : 512) : s.tiles < 256 ? s.tiles : 256);
   return s;
 }
+int64_t stats_floats(const seq_norm_t& p, const Shape& s, int sums) {
+  return s.parts ? s.tiles * s.parts * (s.flat ? p.L : s.cl * 8) * sums : 0;
+}
+int64_t partial_floats(const seq_norm_t& p, const Shape& s) {
+  return (int64_t(s.wgs) * (s.flat ? p.L : 1) * 2 * p.D + 3) / 4 * 4;
+}
 
-template <typename T, typename R, bool POST, int NT, int CL>
+template <typename T, typename R, bool POST, int PHASE, int NT, int CL>
 void launch_cl(const NormArgs& a, const Shape& sh, bool bwd, hipStream_t s) {
   constexpr int H = sizeof(R) == 2 ? 4 : 2;
+  const uint32_t wgs = uint32_t(PHASE ? sh.tiles * sh.parts : bwd ? sh.wgs : sh.tiles);
   if (bwd)
-    norm_bwd_kernel<T, R, POST, NT, CL, H><<<dim3(sh.wgs), NT, 0, s>>>(a);
+    norm_bwd_kernel<T, R, POST, PHASE, NT, CL, H><<<dim3(wgs), NT, 0, s>>>(a);
   else
-    norm_fwd_kernel<T, R, POST, NT, CL, H><<<dim3(uint32_t(sh.tiles)), NT, 0, s>>>(a);
+    norm_fwd_kernel<T, R, POST, PHASE, NT, CL, H><<<dim3(wgs), NT, 0, s>>>(a);
 }
-template <typename T, typename R, bool POST, int NT>
+template <typename T, typename R, bool POST, int PHASE, int NT>
 void launch_nt(const NormArgs& a, const Shape& sh, bool bwd, hipStream_t s) {
   if (sh.flat) {
+    const uint32_t wgs = uint32_t(PHASE ? sh.tiles * sh.parts : bwd ? sh.wgs : sh.tiles);
     if (bwd)
-      norm_bwd_flat_kernel<T, R, POST, NT><<<dim3(sh.wgs), NT, 0, s>>>(a);
+      norm_bwd_flat_kernel<T, R, POST, PHASE, NT><<<dim3(wgs), NT, 0, s>>>(a);
     else
-      norm_fwd_flat_kernel<T, R, POST, NT><<<dim3(a.N), NT, 0, s>>>(a);
+      norm_fwd_flat_kernel<T, R, POST, PHASE, NT><<<dim3(wgs), NT, 0, s>>>(a);
     return;
   }
   switch (sh.cl) {
-    case 2: launch_cl<T, R, POST, NT, 2>(a, sh, bwd, s); break;
-    case 4: launch_cl<T, R, POST, NT, 4>(a, sh, bwd, s); break;
-    default: launch_cl<T, R, POST, NT, 8>(a, sh, bwd, s); break;
+    case 2: launch_cl<T, R, POST, PHASE, NT, 2>(a, sh, bwd, s); break;
+    case 4: launch_cl<T, R, POST, PHASE, NT, 4>(a, sh, bwd, s); break;
+    default: launch_cl<T, R, POST, PHASE, NT, 8>(a, sh, bwd, s); break;
   }
 }
 template <typename T, typename R, bool POST>
 int run(const seq_norm_t& p, bool bwd, hipStream_t s) {
   const Shape sh = shape_of(p);
-  if ((sh.flat ? int64_t(p.N) : sh.tiles) * sh.nt > kMaxThreads) return CONV_ERANGE;
+  if (sh.tiles * (sh.parts ? sh.parts : 1) * sh.nt > kMaxThreads) return CONV_ERANGE;
   NormArgs a = {};
   a.N = p.N, a.D = p.D, a.L = p.L, a.eps = p.eps, a.inv_d = 1.f / float(p.D);
   a.x_n = p.x_n, a.x_d = p.x_d, a.gate_n = p.gate_n, a.gate_d = p.gate_d, a.res_n = p.res_n, a.res_d = p.res_d;
@@ -595,16 +685,23 @@ int run(const seq_norm_t& p, bool bwd, hipStream_t s) {
   a.x = p.x, a.weight = p.weight, a.scale = p.scale, a.gate = p.gate, a.residual = p.residual;
   a.out = p.out, a.sum = p.sum, a.dout = p.dout, a.dsum = p.dsum;
   a.dx = p.dx, a.dgate = p.dgate, a.dresidual = p.dresidual;
-  a.partial = static_cast<float*>(p.workspace);
-  a.tiles = uint32_t(sh.tiles), a.row_tiles = uint32_t(sh.row_tiles);
-  if (bwd) {
+  a.tiles = uint32_t(sh.tiles), a.row_tiles = uint32_t(sh.row_tiles), a.parts = sh.parts, a.part = sh.part;
+  const int64_t need = bwd ? norm_bwd_workspace(p) : norm_fwd_workspace(p);
+  if (need) {
     if (!p.workspace) return CONV_ENULL;
-    if (p.workspace_bytes < norm_bwd_workspace(p)) return CONV_ESCRATCH;
+    if (p.workspace_bytes < need) return CONV_ESCRATCH;
   }
-  if (sh.nt == 1024)
-    launch_nt<T, R, POST, 1024>(a, sh, bwd, s);
-  else
-    launch_nt<T, R, POST, 256>(a, sh, bwd, s);
+  a.partial = static_cast<float*>(p.workspace);
+  a.stats = a.partial + (bwd ? partial_floats(p, sh) : 0);
+  if (sh.parts) {
+    launch_nt<T, R, POST, kSums, 256>(a, sh, bwd, s);
+    if (hipGetLastError() != hipSuccess) return CONV_EHIP;
+    launch_nt<T, R, POST, kRest, 256>(a, sh, bwd, s);
+  } else if (sh.nt == 1024) {
+    launch_nt<T, R, POST, kWhole, 1024>(a, sh, bwd, s);
+  } else {
+    launch_nt<T, R, POST, kWhole, 256>(a, sh, bwd, s);
+  }
   if (hipGetLastError() != hipSuccess) return CONV_EHIP;
   if (!bwd) return CONV_OK;
   const int parts = sh.wgs * (sh.flat ? p.L : 1);
@@ -619,9 +716,12 @@ int run_types(const seq_norm_t& p, bool bwd, hipStream_t s) {
 }
 }  // namespace
 
+int64_t norm_fwd_workspace(const seq_norm_t& p) {
+  return stats_floats(p, shape_of(p), 1) * int64_t(sizeof(float));
+}
 int64_t norm_bwd_workspace(const seq_norm_t& p) {
   const Shape sh = shape_of(p);
-  return int64_t(sh.wgs) * (sh.flat ? p.L : 1) * 2 * p.D * int64_t(sizeof(float));
+  return (partial_floats(p, sh) + stats_floats(p, sh, 2)) * int64_t(sizeof(float));
 }
 int launch_norm_fwd(const seq_norm_t& p, bool post, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -373,7 +373,7 @@ PyObject* norm_pre_fwd(PyObject* const* a) {
   p.residual = strided(c, a[2], "residual", rt, &p.res_n, &p.res_d);
   const Tensor out = c.out(a[5], x.sizes(), c.type()), sum = c.empty(x.sizes(), rt);
   p.out = out.data_ptr(), p.sum = sum.data_ptr();
-  c.run("norm_pre_fwd", seq_norm_pre_fwd, p);
+  c.run("norm_pre_fwd", seq_norm_pre_fwd, p, seq_norm_fwd_workspace);
   return wrap({out, sum});
 }
 
@@ -409,7 +409,7 @@ PyObject* norm_post_fwd(PyObject* const* a) {
   p.residual = strided(c, a[3], "residual", rt, &p.res_n, &p.res_d);
   const Tensor out = c.out(a[6], x.sizes(), rt);
   p.out = out.data_ptr();
-  c.run("norm_post_fwd", seq_norm_post_fwd, p);
+  c.run("norm_post_fwd", seq_norm_post_fwd, p, seq_norm_fwd_workspace);
   return wrap(out);
 }
 

@@ -61,7 +61,7 @@ def norm(**kw):
 
 def test_every_declared_symbol_is_exported():
     fns = re.findall(r"^\s*(?:int|int64_t)\s+(seq_\w+)\s*\(", header(), flags=re.M)
-    assert len(fns) == 14
+    assert len(fns) == 15
     nm = subprocess.run(["nm", "-D", "--defined-only", B.LIB_PATH], capture_output=True, text=True)
     for f in fns:
         assert hasattr(B.lib(), f)
@@ -167,7 +167,8 @@ NORMS = ("seq_norm_pre_fwd", "seq_norm_post_fwd", "seq_norm_pre_bwd", "seq_norm_
 def test_norm_refusals(bad, status):
     for fn in NORMS:
         assert call(fn, norm(**bad)) == status
-    assert call("seq_norm_bwd_workspace", norm(**bad), True) == status
+    for fn in ("seq_norm_fwd_workspace", "seq_norm_bwd_workspace"):
+        assert call(fn, norm(**bad), True) == status
 
 
 def test_norm_combinations():
@@ -192,6 +193,13 @@ def test_norm_combinations():
         assert n > 0 and call(fn, p) == B.CONV_ENULL
         p.workspace, p.workspace_bytes = FAKE, n - 1
         assert call(fn, p) == B.CONV_ESCRATCH
+    for L in (4, 40):  # few columns of many channels: cut into parts
+        p = norm(D=9000, L=L)
+        n = call("seq_norm_fwd_workspace", p, True)
+        assert n > 0 and call("seq_norm_pre_fwd", p) == B.CONV_ENULL
+        p.workspace, p.workspace_bytes = FAKE, n - 1
+        assert call("seq_norm_post_fwd", p) == B.CONV_ESCRATCH
+    assert call("seq_norm_fwd_workspace", norm(N=64, D=9000, L=400), True) == 0
 
 
 def test_python_refuses_what_is_not_on_the_gpu():

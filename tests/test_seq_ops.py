@@ -291,6 +291,12 @@ NORM = [  # N, D, L, dtype, residual dtype, residual, scale, gate, sliced
     (2, 4100, 40, F32, F32, True, True, True, False),
     (30, 20, 600, BF, F32, True, True, False, False),
     (2, 9000, 17, BF, BF, False, False, False, False),
+    (1, 2600, 5, BF, F32, True, True, True, True),
+    (2, 1100, 15, F32, F32, True, True, True, False),
+    (3, 4097, 1, BF, BF, True, True, True, False),
+    (2, 1100, 129, F32, F32, True, True, True, True),
+    (200, 300, 3, BF, BF, True, True, True, False),
+    (600, 30, 2, F32, F32, True, True, True, False),
 ]
 
 
