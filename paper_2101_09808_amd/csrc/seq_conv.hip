@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(const ConvArgs<T> a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = 0.f;
   }
-  store8(a.out + int64_t(row) * a.L + t0, a.L - t0, v);
+  store8<true>(a.out + int64_t(row) * a.L + t0, a.L - t0, v);
   // the thread of the last step (of an empty sequence: the first thread)
   const int last = len > 0 ? len - 1 : 0;
   if (R > 1 && a.final_state && t0 == last / 8 * 8) {
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(const ConvArgs<T> a) {
         if (dfin && k >= 0 && k < R - 1) g[j] += to_f(dfin[k]);
         if (!kInside && t0 + j >= len) g[j] = 0.f;
       }
-      store8(dx + t0, a.L - t0, g);
+      store8<true>(dx + t0, a.L - t0, g);
       if (R > 1 && t0 == 0 && a.dinitial) {
 #pragma unroll
         for (int i = 0; i < R - 1; ++i) {

@@ -180,7 +180,6 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
       }
     };
     auto first = [&](const float* v, int d) {
-      if (PHASE == kRest) return;
       if (!POST && a.sum) store8(static_cast<R*>(a.sum) + base + int64_t(d) * a.L, IN ? 8 : nv, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[0][j] = __builtin_fmaf(v[j], v[j], s[0][j]);
@@ -199,6 +198,7 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
       }
       store8(static_cast<Out*>(a.out) + base + int64_t(d) * a.L, IN ? 8 : nv, o);
     };
+    // (of the residual what the first pass needs: before a block)
     Raw8<T> x[H], g[H];
     Raw8<R> r[H];
 #pragma unroll
@@ -206,16 +206,17 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
       const int d = d0 + k * RS, dc = d < rows ? d : rows - 1;
       x[k] = cols<IN, T>(xp, dc, a.x_d, nv);
       g[k] = has_g ? cols<IN, T>(gp, dc, a.gate_d, nv) : Raw8<T>{};
-      r[k] = has_r ? cols<IN, R>(rp, dc, a.res_d, nv) : Raw8<R>{};
+      r[k] = !POST && has_r ? cols<IN, R>(rp, dc, a.res_d, nv) : Raw8<R>{};
     }
-    float held[H][8];
 #pragma unroll
     for (int k = 0; k < H; ++k) {
       const int d = d0 + k * RS;
-      if (d < rows) {
-        terms(x[k], g[k], r[k], d, held[k]);
-        first(held[k], d);
+      if (PHASE != kRest && d < rows) {
+        float v[8];
+        terms(x[k], g[k], r[k], d, v);
+        first(v, d);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
     auto again_at = [&](int d, float* v, Raw8<R>& rr) {
       const Raw8<T> xx = cols<IN, T>(xp, d, a.x_d, nv), gg = has_g ? cols<IN, T>(gp, d, a.gate_d, nv) : Raw8<T>{};
@@ -239,10 +240,22 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
     d0 = fresh(d0);
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[0][j] = __builtin_amdgcn_rsqf(__builtin_fmaf(s[0][j], a.inv_d, a.eps));
+    if (POST) {
+#pragma unroll
+      for (int k = 0; k < H; ++k) {
+        const int d = d0 + k * RS;
+        r[k] = has_r ? cols<IN, R>(rp, d < rows ? d : rows - 1, a.res_d, nv) : Raw8<R>{};
+      }
+    }
 #pragma unroll
     for (int k = 0; k < H; ++k) {
       const int d = d0 + k * RS;
-      if (d < rows) second(held[k], r[k], d);
+      if (d < rows) {
+        float v[8];
+        terms(again(x[k]), again(g[k]), POST ? r[k] : again(r[k]), d, v);
+        second(v, r[k], d);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // (one channel's registers at a time)
     }
     for (int d = d0 + H * RS; d < rows; d += RS) {
       float v[8];
@@ -620,24 +633,38 @@ Shape shape_of(const seq_norm_t& p) {
     s.nt = int64_t(p.D) * p.L > 2048 ? 1024 : 256;
     s.part = 256 / p.L * 8;
   } else {
-    // Wide tiles use whole cache lines, but every CU should have one, and a
-    // thread's channels should mostly stay in registers.  Forward and backward
-    // with CL = 2, 4, 8: 80 us at 4 for bf16 4 x 2048 x 2048 (256 tiles; 86 at 2,
-    // 100 at 8), 59 us at 2 for fp32 3 x 1000 x 1333 (252 tiles; 80 at 4).
-    s.cl = 8;
-    const auto narrow = [&] { return p.L <= s.cl * 4 || int64_t(p.D) * s.cl > 8192; };
-    while (s.cl > 2 && (narrow() || p.N * ceil_div(p.L, s.cl * 8) < 256)) s.cl /= 2;
+    const auto tile = [&](int cl) {
+      s.cl = cl;
+      s.row_tiles = ceil_div(p.L, cl * 8);
+      s.tiles = s.row_tiles * p.N;
+      s.part = 256 / cl * held(p);
+    };
+    // Whole channels at once where each CU has a tile of at least 32 columns
+    // (whole cache lines of bf16) and half of its channels stay in registers;
+    // else cut.  Forward and backward, whole (at CL 2 or 4) and cut (at 8):
+    // bf16 4 x 2048 x 2048 105 and 105 us, fp32 3 x 1000 x 1333 66 and 59,
+    // bf16 9 x 2816 x 53 110 and 45.
+    tile(p.L > 32 ? 8 : p.L > 16 ? 4 : 2);
+    const auto whole = [&] { return s.tiles >= 256 && int64_t(p.D) * s.cl <= 8192; };
+    if (!whole() && s.cl == 8) {
+      tile(4);
+      if (!whole()) tile(8);
+    }
     s.nt = int64_t(p.D) * s.cl > 512 ? 1024 : 256;
-    s.row_tiles = ceil_div(p.L, s.cl * 8);
-    s.tiles = s.row_tiles * p.N;
-    s.part = 256 / s.cl * held(p);
+    if (whole()) {
+      s.wgs = 256;
+      return s;
+    }
   }
-  // Cut where under half of the CUs would have work and a part is well below
-  // all channels.  bf16 9 x 2816 x 53, forward and
-  // backward: 110 us whole, 45 cut.
-  if (s.tiles < 128 && p.D >= 2 * s.part) {
+  if (p.D >= 2 * s.part && (!s.flat || s.tiles < 128)) {
     s.nt = 256;
     s.parts = int(ceil_div(p.D, s.part));
+  } else {
+    while (s.cl > 2 && s.tiles < 256) {
+      s.cl /= 2;
+      s.row_tiles = ceil_div(p.L, s.cl * 8);
+      s.tiles = s.row_tiles * p.N;
+    }
   }
   s.wgs = int(s.parts ? s.tiles : s.flat ? (s.tiles < 512 ? s.tiles : 512) : s.tiles < 256 ? s.tiles : 256);
   return s;
@@ -656,7 +683,7 @@ void launch_cl(const NormArgs& a, const Shape& sh, bool bwd, hipStream_t s) {
   if (bwd)
     norm_bwd_kernel<T, R, POST, PHASE, NT, CL, H><<<dim3(wgs), NT, 0, s>>>(a);
   else
-    norm_fwd_kernel<T, R, POST, PHASE, NT, CL, H><<<dim3(wgs), NT, 0, s>>>(a);
+    norm_fwd_kernel<T, R, POST, PHASE, NT, CL, PHASE ? H : 2 * H><<<dim3(wgs), NT, 0, s>>>(a);
 }
 template <typename T, typename R, bool POST, int PHASE, int NT>
 void launch_nt(const NormArgs& a, const Shape& sh, bool bwd, hipStream_t s) {

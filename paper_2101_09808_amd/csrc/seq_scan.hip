@@ -766,10 +766,15 @@ __device__ __forceinline__ void each(std::integral_constant<int, N> n, F f) {
   }
 }
 
-// The first m of four floats (or elements that lie `step` apart).
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+// The first m of four floats.  STREAM: past the caches, for what is read once.
+template <bool STREAM>
 __device__ __forceinline__ void load4(const float* p, int m, float* v) {
   if (m == 4) {
-    __builtin_memcpy(v, p, 16);
+    const f32x4u* q = reinterpret_cast<const f32x4u*>(p);
+    const f32x4u r = STREAM ? __builtin_nontemporal_load(q) : *q;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = r[j];
   } else {
 #pragma unroll
     for (int j = 0; j < 3; ++j)
@@ -791,25 +796,39 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
   float A2[CH][4] = {};
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    if (c < have) load4(a.A + int64_t(d0 + c) * a.S + s0, m, A2[c]);
+    if (c < have) load4<false>(a.A + int64_t(d0 + c) * a.S + s0, m, A2[c]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) A2[c][j] *= kLog2e;
   }
   const float bias = a.bias ? a.bias[d] : 0.f, skip = a.Dskip ? a.Dskip[d] : 0.f;
-  for (int n = n0; n < n1; ++n) {
+  struct Token {
+    float h[CH][4], u, delta, z, B[4], C[4];
+  };
+  auto load = [&](int n) {
+    Token t = {};
     const int64_t at = (int64_t(n) * a.D + d0) * a.S + s0;
-    float h[CH][4] = {}, y[CH], B[4] = {}, C[4] = {};
 #pragma unroll
     for (int c = 0; c < CH; ++c)
-      if (c < have) load4(a.initial + at + c * a.S, m, h[c]);
-    const float u = to_f(a.u[n * a.u_n + d * a.u_d]);
-    float dt = to_f(a.delta[n * a.delta_n + d * a.delta_d]) + bias;
-    const float z = a.z ? to_f(a.z[n * a.z_n + d * a.z_d]) : 0.f;
+      if (c < have) load4<true>(a.initial + at + c * a.S, m, t.h[c]);
+    t.u = to_f(a.u[n * a.u_n + d * a.u_d]);
+    t.delta = to_f(a.delta[n * a.delta_n + d * a.delta_d]);
+    if (a.z) t.z = to_f(a.z[n * a.z_n + d * a.z_d]);
     const T* Bp = a.B + n * a.B_n + g * a.B_g + s0 * a.B_s;
     const T* Cp = a.C + n * a.C_n + g * a.C_g + s0 * a.C_s;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (j < m) B[j] = to_f(Bp[j * a.B_s]), C[j] = to_f(Cp[j * a.C_s]);
+      if (j < m) t.B[j] = to_f(Bp[j * a.B_s]), t.C[j] = to_f(Cp[j * a.C_s]);
+    return t;
+  };
+  Token next = load(n0);
+  for (int n = n0; n < n1; ++n) {
+    Token t = next;
+    if (n + 1 < n1) next = load(n + 1);
+    const int64_t at = (int64_t(n) * a.D + d0) * a.S + s0;
+    auto &h = t.h;
+    auto &B = t.B, &C = t.C;
+    const float u = t.u, z = t.z;
+    float y[CH], dt = t.delta + bias;
     if (a.softplus) dt = softplus(dt);
     const float x = dt * u;
     each(std::integral_constant<int, CH>{}, [&](auto ic) {
@@ -824,7 +843,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
       if (c < have) {
         float* to = a.final_state + at + c * a.S;
         if (m == 4) {
-          __builtin_memcpy(to, h[c], 16);
+          __builtin_nontemporal_store(f32x4u{h[c][0], h[c][1], h[c][2], h[c][3]}, reinterpret_cast<f32x4u*>(to));
         } else {
 #pragma unroll
           for (int j = 0; j < 3; ++j)
