@@ -3,21 +3,24 @@
 //   h[s](t) = a[s](t) h[s](t-1) + x(t) B[s](t),  a = exp(dt A[s]),  x = dt u
 //   y(t) = sum_s C[s](t) h[s](t) + Dskip u(t),   out = y z sigmoid(z)
 //
-// A step of a state is an exponential (four times the price of a product) and
-// about five multiply-adds, S of them for every element read: bound by the
-// vector ALU.  The recurrence is composed along the length: a row of sixteen
-// lanes takes a chunk of 128 steps of one channel, eight steps a lane.  Each
-// lane folds its steps (state from zero, and the decay over them), the pairs
-// (decay, state) are scanned over the row by DPP in four levels, and each lane
-// runs its eight steps again from the state that reaches it.  So a step's
-// exponential and products are formed once, the scan costs an eighth of its
-// sixteen instructions a step, and nothing but dt, x and y of eight steps is
-// held over the states.  A wave is four channels, a workgroup 4 NW of one
-// group: they share B and C, staged in LDS as fp32, the next chunk's under way
-// meanwhile.  Workgroups walk along the length.  Where rows are too few to fill
-// the chip the length is cut into segments: a first kernel finds what each
-// segment alone makes of a zero state, the second composes those before its
-// own.
+// A step of a state is an exponential (two issue slots) and five products and
+// multiply-adds, S of them for every element read: bound by the vector ALU.
+// The recurrence is composed along the length.  A row of sixteen lanes takes a
+// channel, 8 or 16 steps a lane; each lane folds its steps (state from zero,
+// and the decay over them), the pairs (decay, state) are scanned over the row
+// by DPP in four levels, and each lane runs its steps again from the state that
+// reaches it.  So a step's exponential and products are formed once, the scan
+// costs a lane eight instructions, and only dt, x and y of the lane's steps are
+// held over the states, which go two at a time.  A wave is four channels; a
+// workgroup's channels are of one group and share B and C, staged in LDS as
+// fp32, the next pass's under way meanwhile.  Workgroups walk along the length.
+// Where rows are too few to fill the chip, a channel has all 64 lanes (short
+// lengths), or the length is cut into segments: a first launch finds what each
+// segment alone makes of a zero state, the second composes those before its own.
+//
+// Forward, bf16, 4 x 2048 x 2048 with 16 states and gate (2^28 steps of states):
+// 80 us, 10.4 issue slots a step of a state (7 of them the recurrence itself),
+// slots in use 82% of the time.  1 x 1024 x 16384 (2^28 too, cut into 8): 150 us.
 #include <type_traits>
 
 #include "seq_device.h"
@@ -409,6 +412,11 @@ __device__ __forceinline__ f32x4 sum_rows(const float* lo, const float* hi) {
 // dC are sums over channels: over a wave's four by permlane swaps, over the
 // workgroup's waves through LDS (two states at a time), over workgroups and
 // segments by scan_sum_kernel from `part_bc`, always in the same order.
+//
+// 4 x 2048 x 2048 with 16 states: 250 us, 28 issue slots a step of a state
+// (in use 87% of the time): 17 the formulas, 4 the scans, 3 the sums over the
+// wave, the rest an element's functions shared by its 16 states; the parts of
+// dB and dC are another 14 us.
 // ENDS: only r of the segment alone at its left end, and its sum of dt.
 template <typename T, int NB, bool GATE, bool ENDS>
 __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
@@ -873,7 +881,9 @@ Shape shape_of(const seq_scan_t& p, bool bwd) {
   const int64_t waves4 = int64_t(p.N) * p.G * ceil_div(s.per, 4);
   s.rows = 4, s.steps = 8;
   if (bwd) {
-    s.waves = s.per > 16 ? 8 : 4;
+    // (larger workgroups leave fewer parts of dB and dC, smaller ones start sooner:
+    // 2 x 520 x 1001 fp32, forward and backward, 52 us at eight waves, 51 at four)
+    s.waves = s.per > 16 && (waves4 > 1024 || s.chunks > 8) ? 8 : 4;
   } else {
     // Few and short rows: a channel has a whole wave, 512 steps a pass (which
     // fits in LDS for up to 16 states).  2 x 520 x 1001: 15 us, against 22 in
@@ -1026,8 +1036,8 @@ int step(const seq_scan_t& p, hipStream_t st) {
   while (lanes * 4 < p.S) lanes *= 2;
   a.blks = int(ceil_div(a.per, lanes < 4 ? lanes : 4));
   // A group takes up to four sequences (A is read once for them) while 4096
-  // waves are left.  256 x 4096 x 16 states: 34 us at one, 30 at two, 28 at four,
-  // 31 at eight.
+  // waves are left.  256 x 4096 x 16 states, from memory: 41 us at one, 39 at two,
+  // 36 at four and at eight, 42 at sixteen.
   const int64_t groups = int64_t(p.N) * p.G * a.blks, waves = groups * lanes / 64;
   a.seqs = waves >= 4 * 4096 ? 4 : waves >= 2 * 4096 ? 2 : 1;
   const int64_t used = ceil_div(p.N, a.seqs) * p.G * a.blks;
