@@ -102,9 +102,9 @@ __device__ __forceinline__ Raw8<T> pack8(const float* v) {
 }
 
 // Stores the first `valid` of eight elements.  STREAM: past the caches, where
-// whole cache lines are written that nothing reads soon (256 x 4096 x 16 states
-// of single tokens 41 -> 38 us); lines that several stores fill have to meet in
-// the L2 (norms: twice as long without).
+// whole cache lines are written that nothing reads soon (the convolution's
+// training step 80 -> 77 us); lines that several stores fill have to meet in the
+// L2 (norms: twice as long without).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
 template <bool STREAM = false, typename T>
 __device__ __forceinline__ void store8(T* p, int valid, const float* v) {

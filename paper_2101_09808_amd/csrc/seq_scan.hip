@@ -734,15 +734,15 @@ __global__ __launch_bounds__(256) void scan_sum_kernel(const ScanArgs<T> a, uint
 }
 
 // One token: bound by the states, which go through memory once, as they lie:
-// four states a lane, GL lanes a channel.  A group of GL lanes has up to four
-// channels; each lane forms one's step and gate (a softplus is as much work as
-// three states) and hands them round, and keeps its A for all the sequences
-// that it works on.
+// four states a lane, GL lanes a channel, so that a wave's store covers whole
+// cache lines.  A group of GL lanes has up to four channels, 64 / GL apart; each
+// lane forms one's step and gate (a softplus is as much work as three states)
+// and hands them round, and keeps its A for all the sequences that it works on.
 template <typename T>
 struct StepArgs {
   int N, D, S, per, G, softplus;
-  int blks, seqs;   // lane groups of a channel group; sequences of a lane group
-  uint32_t groups;  // lane groups
+  int blks, seqs;  // waves of a channel group; sequences of a wave
+  uint32_t waves;
   int64_t u_n, u_d, delta_n, delta_d, z_n, z_d, B_n, B_g, B_s, C_n, C_g, C_s;
   const T *u, *delta, *z, *B, *C;
   const float *A, *Dskip, *bias, *initial;
@@ -792,19 +792,21 @@ __device__ __forceinline__ void load4(const float* p, int m, float* v) {
 
 template <typename T, int GL>
 __global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
-  constexpr int CH = GL < 4 ? GL : 4;  // channels of a lane group
-  const uint32_t lane = blockIdx.x * 256 + threadIdx.x, group = lane / GL;
-  if (group >= a.groups) return;
-  const int li = int(lane % GL), s0 = li * 4, m = a.S - s0 < 0 ? 0 : a.S - s0 < 4 ? a.S - s0 : 4;
-  const uint32_t q = group / uint32_t(a.blks), blk = group - q * a.blks;
+  constexpr int CH = GL < 4 ? GL : 4, W = 64 / GL;  // channels of a lane group, lane groups
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (wave >= a.waves) return;
+  const int lane = threadIdx.x & 63, li = lane % GL, s0 = li * 4, m = a.S - s0 < 0 ? 0 : a.S - s0 < 4 ? a.S - s0 : 4;
+  const uint32_t q = wave / uint32_t(a.blks), blk = wave - q * a.blks;
   const int g = int(q % uint32_t(a.G)), n0 = int(q / uint32_t(a.G)) * a.seqs;
   const int n1 = n0 + a.seqs < a.N ? n0 + a.seqs : a.N;
-  const int have = a.per - int(blk) * CH < CH ? a.per - int(blk) * CH : CH, d0 = g * a.per + int(blk) * CH;
-  const int mine = li < have ? li : have - 1, d = d0 + mine;  // whose scalars this lane forms
+  const int c0 = int(blk) * (CH * W) + lane / GL, left = (a.per - c0 + W - 1) / W, have = left < CH ? left : CH;
+  if (have <= 0) return;  // (a whole lane group)
+  const int d0 = g * a.per + c0;
+  const int mine = li < have ? li : have - 1, d = d0 + mine * W;  // whose scalars this lane forms
   float A2[CH][4] = {};
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    if (c < have) load4<false>(a.A + int64_t(d0 + c) * a.S + s0, m, A2[c]);
+    if (c < have) load4<false>(a.A + int64_t(d0 + c * W) * a.S + s0, m, A2[c]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) A2[c][j] *= kLog2e;
   }
@@ -817,7 +819,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
     const int64_t at = (int64_t(n) * a.D + d0) * a.S + s0;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
-      if (c < have) load4<true>(a.initial + at + c * a.S, m, t.h[c]);
+      if (c < have) load4<true>(a.initial + at + int64_t(c * W) * a.S, m, t.h[c]);
     t.u = to_f(a.u[n * a.u_n + d * a.u_d]);
     t.delta = to_f(a.delta[n * a.delta_n + d * a.delta_d]);
     if (a.z) t.z = to_f(a.z[n * a.z_n + d * a.z_d]);
@@ -849,7 +851,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
         y[c] = __builtin_fmaf(C[j], h[c][j], y[c]);
       }
       if (c < have) {
-        float* to = a.final_state + at + c * a.S;
+        float* to = a.final_state + at + int64_t(c * W) * a.S;
         if (m == 4) {
           __builtin_nontemporal_store(f32x4u{h[c][0], h[c][1], h[c][2], h[c][3]}, reinterpret_cast<f32x4u*>(to));
         } else {
@@ -1023,9 +1025,7 @@ int bwd(const seq_scan_t& p, hipStream_t st) {
 
 template <typename T, int GL>
 int step_launch(const StepArgs<T>& a, hipStream_t st) {
-  const int64_t wgs = ceil_div(int64_t(a.groups) * GL, 256);
-  if (wgs * 256 > kMaxThreads) return CONV_ERANGE;
-  scan_step_kernel<T, GL><<<dim3(uint32_t(wgs)), 256, 0, st>>>(a);
+  scan_step_kernel<T, GL><<<dim3((a.waves - 1) / 4 + 1), 256, 0, st>>>(a);
   return hipGetLastError() == hipSuccess ? CONV_OK : CONV_EHIP;
 }
 template <typename T>
@@ -1034,15 +1034,15 @@ int step(const seq_scan_t& p, hipStream_t st) {
   a.N = p.N, a.D = p.D, a.S = p.S, a.G = p.G, a.per = p.D / p.G, a.softplus = p.delta_softplus;
   int lanes = 1;
   while (lanes * 4 < p.S) lanes *= 2;
-  a.blks = int(ceil_div(a.per, lanes < 4 ? lanes : 4));
-  // A group takes up to four sequences (A is read once for them) while 4096
-  // waves are left.  256 x 4096 x 16 states, from memory: 41 us at one, 39 at two,
-  // 36 at four and at eight, 42 at sixteen.
-  const int64_t groups = int64_t(p.N) * p.G * a.blks, waves = groups * lanes / 64;
+  a.blks = int(ceil_div(a.per, 64 / lanes * (lanes < 4 ? lanes : 4)));
+  // A wave takes up to four sequences (A is read once for them) while 4096 waves
+  // are left.  256 x 4096 x 16 states, from memory: 33 us at one, 32 at two, 31 at
+  // four, 33 at eight (140 MB: 4.5 TB/s).
+  const int64_t waves = int64_t(p.N) * p.G * a.blks;
   a.seqs = waves >= 4 * 4096 ? 4 : waves >= 2 * 4096 ? 2 : 1;
   const int64_t used = ceil_div(p.N, a.seqs) * p.G * a.blks;
-  if (used * lanes > kMaxThreads) return CONV_ERANGE;
-  a.groups = uint32_t(used);
+  if ((used + 3) * 64 > kMaxThreads) return CONV_ERANGE;
+  a.waves = uint32_t(used);
   a.u_n = p.u_n, a.u_d = p.u_d, a.delta_n = p.delta_n, a.delta_d = p.delta_d, a.z_n = p.z_n, a.z_d = p.z_d;
   a.B_n = p.B_n, a.B_g = p.B_g, a.B_s = p.B_s, a.C_n = p.C_n, a.C_g = p.C_g, a.C_s = p.C_s;
   const auto t = [](const void* v) { return static_cast<const T*>(v); };
