@@ -126,9 +126,16 @@ def selective_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_sof
         x = (dt[..., t] * u[..., t])[..., None] * B[..., t]
         h = a * h + x
         m = a * m + x.abs()
-        # a: the product's rounding and dt's (16 half steps, relative to the
-        # exponent), one step of exp2; x: four products; the sum's rounding
-        err = a * err + m * (8 + 16 * (A * dt[..., t, None]).abs())
+        # In steps of 2^-24.  dt: without softplus one rounding; through it, for
+        # v = raw far below zero, dt is about e = exp(v), whose relative error is
+        # |v| for v's own rounding, 1.3 |v| for its product with log2(e) and that
+        # constant, and 10 for exp2, the reciprocal, three products, the
+        # polynomial and the last sum; for v above zero e's part of dt shrinks.
+        # a: the exponent's relative error (dt's, A's product with the constant,
+        # the product, a sum over dt) times the exponent, 2 for exp2.  x: dt's
+        # and three products.  The state: products and sums of the composition.
+        edt = 2.5 * raw[..., t].abs() + 10 if delta_softplus else torch.ones_like(dt[..., t])
+        err = a * err + m * (8 + (8 + edt[..., None]) * (A * dt[..., t, None]).abs()) + x.abs() * edt[..., None]
         ys.append((h * C[..., t]).sum(-1))
         ms.append((m * C[..., t].abs()).sum(-1))
         es.append((err * C[..., t].abs()).sum(-1))

@@ -941,14 +941,15 @@ int launch(K kernel, int64_t wgs, int threads, int64_t lds, hipStream_t s, const
   kernel<<<dim3(uint32_t(wgs)), threads, uint32_t(lds), s>>>(a);
   return hipGetLastError() == hipSuccess ? CONV_OK : CONV_EHIP;
 }
-// Staging loads of 16 bytes (fp32: 32) a thread holds for the next pass.
-template <typename F>
+// Staging loads of 16 bytes (fp32: 32) a thread holds for the next pass: 1, 2, 4
+// or 8, at most MOST.
+template <int MOST, int NB = 1, typename F>
 int with_loads(int rows, int pass, int waves, F f) {
-  const int64_t nb = ceil_div(rows * pass / 8, waves * 64);
-  if (nb <= 1) return f(std::integral_constant<int, 1>{});
-  if (nb <= 2) return f(std::integral_constant<int, 2>{});
-  if (nb <= 4) return f(std::integral_constant<int, 4>{});
-  return f(std::integral_constant<int, 8>{});
+  if (ceil_div(rows * pass / 8, waves * 64) > NB) {
+    if constexpr (NB < MOST) return with_loads<MOST, 2 * NB>(rows, pass, waves, f);
+    return CONV_ENOPLAN;
+  }
+  return f(std::integral_constant<int, NB>{});
 }
 
 template <typename T, int RW, int TS, bool ENDS>
@@ -957,7 +958,8 @@ int fwd_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st)
   constexpr int pass = 64 / RW * TS, per = ENDS ? 1 : pass / kChunk;
   const int rows = ENDS ? p.S : 2 * p.S;
   const int64_t lds = ((2 * rows + 1) * int64_t(pass) + s.waves * (1 + per) * RW * ((p.S + 1) & ~1)) * 4;
-  return with_loads(rows, pass, s.waves, [&](auto nb) {
+  // (512 steps of 32 rows by 4 waves; else 256 of 32 or 128 of 64 by 4, 128 of 128 by 8)
+  return with_loads<(RW == 1 ? 8 : 4) / (ENDS ? 2 : 1)>(rows, pass, s.waves, [&](auto nb) {
     return launch(scan_fwd_kernel<T, RW, TS, decltype(nb)::value, ENDS>, s.wgs / s.segs * a.run_segs, s.waves * 64, lds, st, a);
   });
 }
@@ -990,7 +992,7 @@ int bwd_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st)
   const int rows = ENDS ? p.S : 2 * p.S, Se = (p.S + 1) & ~1;
   const int64_t lds =
       ((rows + 1) * int64_t(kChunk) + (ENDS ? 0 : a.batch * s.waves * 256) + s.waves * (ENDS ? 8 : 16) * Se) * 4;
-  return with_loads(rows, kChunk, s.waves, [&](auto nb) {
+  return with_loads<ENDS ? 4 : 8>(rows, kChunk, s.waves, [&](auto nb) {
     return launch(scan_bwd_kernel<T, decltype(nb)::value, GATE, ENDS>, s.wgs / s.segs * a.run_segs, s.waves * 64, lds, st, a);
   });
 }

@@ -199,7 +199,7 @@ def test_norm_combinations():
         assert n > 0 and call("seq_norm_pre_fwd", p) == B.CONV_ENULL
         p.workspace, p.workspace_bytes = FAKE, n - 1
         assert call("seq_norm_post_fwd", p) == B.CONV_ESCRATCH
-    assert call("seq_norm_fwd_workspace", norm(N=64, D=9000, L=400), True) == 0
+    assert call("seq_norm_fwd_workspace", norm(N=64, D=900, L=400), True) == 0
 
 
 def test_python_refuses_what_is_not_on_the_gpu():
