@@ -898,8 +898,13 @@ Shape shape_of(const seq_scan_t& p, bool bwd) {
   // for waves (two a SIMD) take at once.
   const int64_t wgs = int64_t(p.N) * p.G * s.blks, places = 2048 / s.waves;
   int64_t want = wgs * s.waves <= (bwd || s.rows == 1 ? 1024 : 512) ? places / wgs : 1;
-  // 16 steps a lane are a sixth less work a step, but a pass may waste twice as many.
-  if (!bwd && s.rows == 4 && p.S <= 16 && ceil_div(p.L, 256) * 12 <= ceil_div(p.L, 128) * 7 && want * 256 <= p.L)
+  // 16 steps a lane are a sixth less work, but a pass may waste twice as many,
+  // and two waves fit on a SIMD instead of three: for a chip that two a SIMD fill
+  // at once (4 x 2048 x 2048, forward and backward, 348 us against 355; 1 x 1024 x
+  // 16384 150 against 160), and long rows (ragged 6 x 1536 x 4000 155 against 173;
+  // ragged 12 x 4096 x 700, however, 164 against 131).
+  if (!bwd && s.rows == 4 && p.S <= 16 && ceil_div(p.L, 256) * 12 <= ceil_div(p.L, 128) * 7 && want * 256 <= p.L &&
+      (wgs * s.waves * want <= 2048 || p.L > 2048))
     s.steps = 16;
   const int per = 64 / s.rows * s.steps / kChunk;  // chunks a pass
   const int64_t passes = ceil_div(s.chunks, per);
