@@ -212,14 +212,13 @@ __device__ __forceinline__ int64_t state_at(const ScanArgs<T>& a, const Place& p
 }
 
 // RW channels a wave, LN = 64 / RW lanes each; TS steps a lane, LN TS a pass.
-// ENDS: only what the segment makes of a zero state, and its sum of dt.
-template <typename T, int RW, int TS, int NB, bool ENDS>
+template <typename T, int RW, int TS, int NB>
 __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
   extern __shared__ float lds[];
   constexpr int LN = 64 / RW, kSteps = LN * TS;
-  constexpr int kPer = ENDS ? 1 : kSteps / kChunk, kLanes = kChunk / TS;  // checkpoints a pass, lanes to one
+  constexpr int kPer = kSteps / kChunk, kLanes = kChunk / TS;  // checkpoints a pass, lanes to one
   const Place p = place<RW>(a);
-  const int S = a.S, Se = (S + 1) & ~1, rows = ENDS ? S : 2 * S, lane = p.lane, row = p.row, tl = p.tl;
+  const int S = a.S, Se = (S + 1) & ~1, rows = 2 * S, lane = p.lane, row = p.row, tl = p.tl;
   const int len = seq_len(a.lengths, p.n, a.L), held = p.held;
   // (a segment is of whole passes)
   const int first = p.seg * a.seg_chunks * kChunk;
@@ -234,10 +233,8 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
     if (r < held && s < S) {
       const int64_t at = state_at(a, p, 0) + int64_t(r) * S + s;
       A2 = kLog2e * a.A[at];
-      if (!ENDS) {
-        if (a.initial) h = a.initial[int64_t(p.n) * a.D * S + at];
-        if (p.seg) h = through(a, p.n, 0, p.seg, 1, at, p.d0 + r, A2, h);
-      }
+      if (a.initial) h = a.initial[int64_t(p.n) * a.D * S + at];
+      if (p.seg) h = through(a, p.n, 0, p.seg, 1, at, p.d0 + r, A2, h);
     }
     as[e] = A2;
     hs[e] = h;
@@ -253,8 +250,7 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
   const T* Bp = a.B + p.n * a.B_n + p.g * a.B_g;
   const T* Cp = a.C + p.n * a.C_n + p.g * a.C_g;
   const float skip = a.Dskip ? a.Dskip[p.d] : 0.f, bias = a.bias ? a.bias[p.d] : 0.f;
-  T* op = ENDS ? nullptr : a.out + (int64_t(p.n) * a.D + p.d) * a.L + tl * TS;
-  float total = 0.f;
+  T* op = a.out + (int64_t(p.n) * a.D + p.d) * a.L + tl * TS;
   Stage<T, LN, TS, NB> st;
   Raw8<T> ru[TS / 8] = {}, rd[TS / 8] = {}, rz[TS / 8] = {};
   auto fetch = [&](const T* from, int t0, Raw8<T>* r) {
@@ -273,7 +269,7 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
     const int valid = len - t0 - tl * TS;
     const float* cur = bc + buf * rows * kSteps;
     const bool more = t0 + kSteps < end, full = t0 + kSteps <= len;
-    if (!ENDS && a.checkpoints)
+    if (a.checkpoints)
       put(a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + t0 / kChunk), hs);
     float dt[TS], x[TS], y[TS];
     const float sum = steps<T, TS>(rd, bias, a.softplus, full, valid, dt);
@@ -289,7 +285,7 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
       fetch(up, t0 + kSteps, ru);
       fetch(dp, t0 + kSteps, rd);
     }
-    if (!ENDS && zp) fetch(zp, t0, rz);
+    if (zp) fetch(zp, t0, rz);
     for (int s = 0; s < S; s += 2) {
       // (with S odd the last state's pair is of decay 1 and reads zeros)
       const bool two = s + 1 < S;
@@ -316,10 +312,6 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) H[i] = __builtin_fmaf(P[i], tl == 0 ? in[i] : 0.f, H[i]);
       scan_lanes<LN>(H, P, in);
-      if (ENDS) {
-        if (tl == LN - 1) hs[row * Se + s] = H[0], hs[row * Se + s + 1] = H[1];
-        continue;
-      }
       float c[2][TS];
       lds_steps<LN, TS>(b0 + S * kSteps, tl, c[0]);
       lds_steps<LN, TS>(two ? b0 + (S + 1) * kSteps : zeros, tl, c[1]);
@@ -336,12 +328,11 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
         to[0] = in[0], to[1] = in[1];
       }
     }
-    total += sum;
     if (kPer > 1 && a.checkpoints) {
       for (int k = 1; k < kPer && t0 + k * kChunk < end; ++k)
         put(a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + t0 / kChunk + k), mid + (k - 1) * RW * Se);
     }
-    if (!ENDS && p.ok) {
+    if (p.ok) {
 #pragma unroll
       for (int k = 0; k < TS / 8; ++k) {
         float* yk = y + 8 * k;
@@ -363,13 +354,6 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
     buf ^= 1;
     __syncthreads();
   }
-  if (ENDS) {
-    const int64_t at = int64_t(p.n) * a.segs + p.seg;
-    put(a.ends + state_at(a, p, at), hs);
-    for (int m = 1; m < LN; m <<= 1) total += __shfl_xor(total, m);
-    if (tl == 0 && p.ok) a.end_dt[at * a.D + p.d] = total;
-    return;
-  }
   if (a.final_state && p.seg == a.segs - 1) put(a.final_state + state_at(a, p, p.n), hs);
   if (p.ok) {  // (passes behind the end)
     const float zero[8] = {};
@@ -379,6 +363,127 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
 #pragma unroll
       for (int k = 0; k < TS / 8; ++k) store8(op + t0 + 8 * k, stop - t0 - tl * TS - 8 * k, zero);
   }
+}
+
+// What a segment alone makes of a zero state, and its sum of dt: forward, h at
+// its right end, the sum of x(t) B(t) exp(A (dt behind t)); BACK, r at its left
+// end, the sum of dy(t) C(t) exp(A (dt up to and with t)).  The steps stand side
+// by side, weighted with their decay to that end, so a state needs no scan, only
+// a sum over the row; the decays' exponents are sums of dt, taken along as the
+// passes walk away from the end.  1 x 1024 x 16384, 16 states, seven segments of
+// eight: ENDS_US us.
+template <typename T, int TS, int NB, bool BACK>
+__global__ __launch_bounds__(512) void scan_ends_kernel(const ScanArgs<T> a) {
+  extern __shared__ float lds[];
+  constexpr int kSteps = 16 * TS;
+  const Place p = place<4>(a);
+  const int S = a.S, Se = (S + 1) & ~1, lane = p.lane, row = p.row, tl = p.tl;
+  const int len = seq_len(a.lengths, p.n, a.L);
+  const int first = p.seg * a.seg_chunks * kChunk;
+  const int stop = p.seg == a.segs - 1 ? a.L : first + a.seg_chunks * kChunk, end = len < stop ? len : stop;
+  const int passes = end > first ? (end - first + kSteps - 1) / kSteps : 0;
+  float* bc = lds;  // [2][S], a row of zeros behind them
+  float* zeros = bc + 2 * S * kSteps;
+  float* hs = zeros + kSteps + p.wave * 8 * Se;
+  float* as = hs + 4 * Se;
+  for (int e = lane; e < 4 * Se; e += 64) {
+    const int r = e / Se, s = e - r * Se;
+    as[e] = r < p.held && s < S ? kLog2e * a.A[state_at(a, p, 0) + int64_t(r) * S + s] : 0.f;
+    hs[e] = 0.f;
+  }
+  for (int e = threadIdx.x; e < kSteps; e += blockDim.x) zeros[e] = 0.f;
+  const bool gate = BACK && a.z;
+  const T* dp = a.delta + p.n * a.delta_n + p.d * a.delta_d + tl * TS;
+  const T* vp = BACK ? a.dout + p.n * a.dout_n + p.d * a.dout_d + tl * TS : a.u + p.n * a.u_n + p.d * a.u_d + tl * TS;
+  const T* zp = gate ? a.z + p.n * a.z_n + p.d * a.z_d + tl * TS : nullptr;
+  const T* Mp = BACK ? a.C + p.n * a.C_n + p.g * a.C_g : a.B + p.n * a.B_n + p.g * a.B_g;
+  const int64_t M_s = BACK ? a.C_s : a.B_s;
+  const float bias = a.bias ? a.bias[p.d] : 0.f;
+  Stage<T, 16, TS, NB> st;
+  Raw8<T> rd[TS / 8] = {}, rv[TS / 8] = {}, rz[TS / 8] = {};
+  auto at_pass = [&](int k) { return first + (BACK ? k : passes - 1 - k) * kSteps; };
+  auto fetch = [&](int t0) {
+    st.load(Mp, M_s, Mp, M_s, S, S, t0, end);
+#pragma unroll
+    for (int k = 0; k < TS / 8; ++k) {
+      const int valid = end - t0 - tl * TS - 8 * k;
+      rd[k] = load8(dp + t0 + 8 * k, valid);
+      rv[k] = load8(vp + t0 + 8 * k, valid);
+      if (gate) rz[k] = load8(zp + t0 + 8 * k, valid);
+    }
+  };
+  if (passes) {
+    fetch(at_pass(0));
+    st.store(bc, S);
+  }
+  __syncthreads();
+  float total = 0.f;  // dt of the passes behind
+  for (int k = 0; k < passes; ++k) {
+    const int t0 = at_pass(k);
+    const float* cur = bc + (k & 1) * S * kSteps;
+    float dt[TS], v[TS];
+    const float sum = steps<T, TS>(rd, bias, a.softplus, t0 + kSteps <= end, end - t0 - tl * TS, dt);
+#pragma unroll
+    for (int i = 0; i < TS / 8; ++i) {
+      unpack8(rv[i], v + 8 * i);
+      if (gate) {
+        float z[8];
+        unpack8(rz[i], z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[8 * i + j] *= z[j] * sigmoid(z[j]);
+      }
+    }
+    if (!BACK) {
+#pragma unroll
+      for (int j = 0; j < TS; ++j) v[j] *= dt[j];
+    }
+    if (k + 1 < passes) fetch(at_pass(k + 1));
+    // dt becomes each step's distance from the end: the lanes' sums first
+    float lanes = sum;
+    if (BACK) {
+      lanes += dpp0<kRowShr + 1>(lanes);
+      lanes += dpp0<kRowShr + 2>(lanes);
+      lanes += dpp0<kRowShr + 4>(lanes);
+      lanes += dpp0<kRowShr + 8>(lanes);
+    } else {
+      lanes += dpp0<kRowShl + 1>(lanes);
+      lanes += dpp0<kRowShl + 2>(lanes);
+      lanes += dpp0<kRowShl + 4>(lanes);
+      lanes += dpp0<kRowShl + 8>(lanes);
+    }
+    float far = total + (BACK ? dpp0<kRowShr + 1>(lanes) : dpp0<kRowShl + 1>(lanes));
+    total += __shfl(lanes, (lane & 48) + (BACK ? 15 : 0));
+    if (BACK) {
+#pragma unroll
+      for (int j = 0; j < TS; ++j) dt[j] = far += dt[j];
+    } else {
+#pragma unroll
+      for (int j = TS - 1; j >= 0; --j) {
+        const float own = dt[j];
+        dt[j] = far;
+        far += own;
+      }
+    }
+    for (int s = 0; s < S; s += 2) {
+      const float *m0 = cur + s * kSteps, *m1 = s + 1 < S ? m0 + kSteps : zeros;
+      float m[2][TS], H[2] = {0.f, 0.f};
+      const float A2[2] = {as[row * Se + s], as[row * Se + s + 1]};
+      lds_steps<16, TS>(m0, tl, m[0]);
+      lds_steps<16, TS>(m1, tl, m[1]);
+#pragma unroll
+      for (int j = 0; j < TS; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) H[i] = __builtin_fmaf(exp2_fast(dt[j] * A2[i]), v[j] * m[i][j], H[i]);
+      H[0] = row_sum(H[0]), H[1] = row_sum(H[1]);
+      if (tl == 15) hs[row * Se + s] += H[0], hs[row * Se + s + 1] += H[1];
+    }
+    if (k + 1 < passes) st.store(bc + ((k + 1) & 1) * S * kSteps, S);
+    __syncthreads();
+  }
+  const int64_t at = int64_t(p.n) * a.segs + p.seg;
+  float* to = a.ends + state_at(a, p, at);
+  for (int e = lane; e < p.held * S; e += 64) to[e] = hs[e + e / S * (Se - S)];
+  if (tl == 0 && p.ok) a.end_dt[at * a.D + p.d] = total;
 }
 
 // Sums sixteen values over the four rows: lane (row, tl) gets, of position tl,
@@ -417,21 +522,20 @@ __device__ __forceinline__ f32x4 sum_rows(const float* lo, const float* hi) {
 // (in use 87% of the time): 17 the formulas, 4 the scans, 3 the sums over the
 // wave, the rest an element's functions shared by its 16 states; the parts of
 // dB and dC are another 14 us.
-// ENDS: only r of the segment alone at its left end, and its sum of dt.
-template <typename T, int NB, bool GATE, bool ENDS>
+template <typename T, int NB, bool GATE>
 __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
   extern __shared__ float lds[];
   const Place p = place<4>(a);
-  const int S = a.S, Se = (S + 1) & ~1, rows = ENDS ? S : 2 * S, lane = p.lane, row = p.row, tl = p.tl;
+  const int S = a.S, Se = (S + 1) & ~1, rows = 2 * S, lane = p.lane, row = p.row, tl = p.tl;
   const int nw = blockDim.x >> 6, batch = a.batch;
   const int len = seq_len(a.lengths, p.n, a.L);
   const int c0 = p.seg * a.seg_chunks, c1 = c0 + a.seg_chunks < a.chunks ? c0 + a.seg_chunks : a.chunks;
   const int used = (len + kChunk - 1) / kChunk, cend = used < c1 ? used : c1;
-  float* bc = lds;                     // B then C (ENDS: C), a row of zeros behind them
+  float* bc = lds;                     // B then C, a row of zeros behind them
   float* zeros = bc + rows * kChunk;
   float* ex = zeros + kChunk;          // [batch][waves][256]
-  float* as = ex + (ENDS ? 0 : batch * nw * 256) + p.wave * (ENDS ? 8 : 16) * Se;
-  float *rs = as + 4 * Se, *hs = rs + 4 * Se, *dAs = hs + 4 * Se;  // (ENDS: the first two)
+  float* as = ex + batch * nw * 256 + p.wave * 16 * Se;
+  float *rs = as + 4 * Se, *hs = rs + 4 * Se, *dAs = hs + 4 * Se;
   const int held = p.held;
   for (int e = lane; e < 4 * Se; e += 64) {
     const int r0 = e / Se, s = e - r0 * Se;
@@ -439,14 +543,12 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
     if (r0 < held && s < S) {
       const int64_t at = state_at(a, p, 0) + int64_t(r0) * S + s;
       A2 = kLog2e * a.A[at];
-      if (!ENDS) {
-        if (a.dfinal) r = a.dfinal[int64_t(p.n) * a.D * S + at];
-        if (p.seg < a.segs - 1) r = through(a, p.n, a.segs - 1, p.seg, -1, at, p.d0 + r0, A2, r);
-      }
+      if (a.dfinal) r = a.dfinal[int64_t(p.n) * a.D * S + at];
+      if (p.seg < a.segs - 1) r = through(a, p.n, a.segs - 1, p.seg, -1, at, p.d0 + r0, A2, r);
     }
     as[e] = A2;
     rs[e] = r;
-    if (!ENDS) hs[e] = dAs[e] = 0.f;
+    hs[e] = dAs[e] = 0.f;
   }
   for (int e = threadIdx.x; e < kChunk; e += blockDim.x) zeros[e] = 0.f;
   const T* up = a.u + p.n * a.u_n + p.d * a.u_d + tl * 8;
@@ -459,26 +561,21 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
   const int64_t at_row = (int64_t(p.n) * a.D + p.d) * a.L + tl * 8;
   // (the steps of a row without a channel are all behind its end: they add nothing)
   const int row_len = p.ok ? len - tl * 8 : 0;
-  float total = 0.f, dD = 0.f, dbias = 0.f;
+  float dD = 0.f, dbias = 0.f;
   Stage<T, 16, 8, NB> st;
   Raw8<T> ru = {}, rd = {}, rz = {}, rg = {};
   float ck[4];  // the chunk's checkpoint: entries lane, lane + 64, ... of [channel][S]
   auto fetch = [&](int c) {
     const int t0 = c * kChunk, valid = row_len - t0;
-    if (ENDS)
-      st.load(Cp, a.C_s, Cp, a.C_s, S, rows, t0, len);
-    else
-      st.load(Bp, a.B_s, Cp, a.C_s, S, rows, t0, len);
-    if (!ENDS) ru = load8(up + t0, valid);
+    st.load(Bp, a.B_s, Cp, a.C_s, S, rows, t0, len);
+    ru = load8(up + t0, valid);
     rd = load8(dp + t0, valid);
     rg = load8(gp + t0, valid);
     if (GATE) rz = load8(zp + t0, valid);
-    if (!ENDS) {
-      const float* from = a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + c);
+    const float* from = a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + c);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (lane + k * 64 < held * S) ck[k] = from[lane + k * 64];
-    }
+    for (int k = 0; k < 4; ++k)
+      if (lane + k * 64 < held * S) ck[k] = from[lane + k * 64];
   };
   int ck_at[4];  // where they belong in [channel][Se]
 #pragma unroll
@@ -504,13 +601,11 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
     const int t0 = c * kChunk, valid = row_len - t0;
     const bool full = t0 + kChunk <= len;
     __syncthreads();  // (the chunk before has been read, its last batch written)
-    if (!ENDS && c + 1 < cend) sum_batch(last, c + 1);
+    if (c + 1 < cend) sum_batch(last, c + 1);
     st.store(bc, rows);
-    if (!ENDS) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (lane + k * 64 < held * S) hs[ck_at[k]] = ck[k];
-    }
+    for (int k = 0; k < 4; ++k)
+      if (lane + k * 64 < held * S) hs[ck_at[k]] = ck[k];
     float dt[8], x[8], dy[8], dx[8], ddt[8], y[8];
     const float sum = steps<T, 8>(&rd, bias, a.softplus, full, valid, dt);
     const Raw8<T> ku = again(ru), kd = again(rd), kg = again(rg), kz = again(rz);
@@ -522,14 +617,12 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) dy[j] *= z[j] * sigmoid(z[j]);
       }
-      if (!ENDS) {
-        unpack8(ru, u);
+      unpack8(ru, u);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          x[j] = dt[j] * u[j];
-          dx[j] = ddt[j] = 0.f;
-          y[j] = skip * u[j];
-        }
+      for (int j = 0; j < 8; ++j) {
+        x[j] = dt[j] * u[j];
+        dx[j] = ddt[j] = 0.f;
+        y[j] = skip * u[j];
       }
     }
     __syncthreads();
@@ -539,7 +632,7 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
     for (int s = 0; s < S; s += 2) {
       const bool two = s + 1 < S;
       const float* b0 = bc + s * kChunk;
-      const float* q0 = ENDS ? b0 : b0 + S * kChunk;
+      const float* q0 = b0 + S * kChunk;
       float b[2][8], cc[2][8], w[2][8], A2[2], rin[2], R[2] = {0.f, 0.f}, P[2], Q[2];
       lds_steps<16, 8>(q0, tl, cc[0]);
       lds_steps<16, 8>(two ? q0 + kChunk : zeros, tl, cc[1]);
@@ -560,10 +653,6 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) R[i] = __builtin_fmaf(P[i], tl == 15 ? rin[i] : 0.f, R[i]);
       scan_lanes_back(R, P, rin);
-      if (ENDS) {
-        if (tl == 0) rs[row * Se + s] = R[0], rs[row * Se + s + 1] = R[1];
-        continue;
-      }
       float* exb = ex + (s & (batch - 1)) * nw * 256 + p.wave * 256 + lane * 4;
       float h[2][8], hin[2], H[2] = {0.f, 0.f}, dA[2] = {0.f, 0.f};
       lds_steps<16, 8>(b0, tl, b[0]);
@@ -617,8 +706,6 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
         __syncthreads();  // (the next batch overwrites it)
       }
     }
-    total += sum;
-    if (ENDS) continue;
     if (p.ok) {
       float u[8], raw[8], o[8], od[8], oz[8];
       unpack8(ku, u);
@@ -657,7 +744,7 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
       if (GATE) store8(a.dz + at_row + t0, room, oz);
     }
   }
-  if (!ENDS && c0 < cend) {
+  if (c0 < cend) {
     __syncthreads();
     sum_batch(last, c0);
   }
@@ -665,12 +752,6 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
   const auto put = [&](float* to, const float* from) {
     for (int e = lane; e < held * S; e += 64) to[e] = from[e + e / S * (Se - S)];
   };
-  if (ENDS) {
-    put(a.ends + state_at(a, p, at), rs);
-    total = row_sum(total);
-    if (tl == 15 && p.ok) a.end_dt[at * a.D + p.d] = total;
-    return;
-  }
   put(a.part_A + state_at(a, p, at), dAs);
   if (a.dinitial && p.seg == 0) put(a.dinitial + state_at(a, p, p.n), rs);
   dD = row_sum(dD), dbias = row_sum(dbias);
@@ -923,7 +1004,7 @@ template <typename T>
 ScanArgs<T> args_of(const seq_scan_t& p, const Shape& s) {
   ScanArgs<T> a = {};
   a.N = p.N, a.D = p.D, a.L = p.L, a.S = p.S, a.G = p.G, a.per = s.per, a.softplus = p.delta_softplus;
-  a.blks = s.blks, a.segs = s.segs, a.seg_chunks = s.seg_chunks, a.chunks = s.chunks;
+  a.blks = s.blks, a.segs = a.run_segs = s.segs, a.seg_chunks = s.seg_chunks, a.chunks = s.chunks;
   a.u_n = p.u_n, a.u_d = p.u_d, a.delta_n = p.delta_n, a.delta_d = p.delta_d, a.z_n = p.z_n, a.z_d = p.z_d;
   a.dout_n = p.dout_n, a.dout_d = p.dout_d;
   a.B_n = p.B_n, a.B_g = p.B_g, a.B_s = p.B_s, a.C_n = p.C_n, a.C_g = p.C_g, a.C_s = p.C_s;
@@ -957,21 +1038,31 @@ int with_loads(int rows, int pass, int waves, F f) {
   return f(std::integral_constant<int, NB>{});
 }
 
-template <typename T, int RW, int TS, bool ENDS>
-int fwd_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st) {
-  a.run_segs = ENDS ? s.segs - 1 : s.segs;  // (nothing comes after the last one's end)
-  constexpr int pass = 64 / RW * TS, per = ENDS ? 1 : pass / kChunk;
-  const int rows = ENDS ? p.S : 2 * p.S;
-  const int64_t lds = ((2 * rows + 1) * int64_t(pass) + s.waves * (1 + per) * RW * ((p.S + 1) & ~1)) * 4;
-  // (512 steps of 32 rows by 4 waves; else 256 of 32 or 128 of 64 by 4, 128 of 128 by 8)
-  return with_loads<(RW == 1 ? 8 : 4) / (ENDS ? 2 : 1)>(rows, pass, s.waves, [&](auto nb) {
-    return launch(scan_fwd_kernel<T, RW, TS, decltype(nb)::value, ENDS>, s.wgs / s.segs * a.run_segs, s.waves * 64, lds, st, a);
+template <typename T, int TS, bool BACK>
+int ends_steps(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, int64_t wgs, hipStream_t st) {
+  const int64_t lds = ((2 * p.S + 1) * int64_t(16 * TS) + 4 * 8 * ((p.S + 1) & ~1)) * 4;
+  return with_loads<4>(p.S, 16 * TS, 4, [&](auto nb) {
+    return launch(scan_ends_kernel<T, TS, decltype(nb)::value, BACK>, wgs, 256, lds, st, a);
   });
 }
-template <typename T, bool ENDS>
-int fwd_kind(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
-  if (s.rows == 1) return fwd_pass<T, 1, 8, ENDS>(p, s, a, st);
-  return s.steps == 16 ? fwd_pass<T, 4, 16, ENDS>(p, s, a, st) : fwd_pass<T, 4, 8, ENDS>(p, s, a, st);
+// The ends of all segments but the last (BACK: the first), which nothing comes after.
+template <typename T, bool BACK>
+int ends_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st) {
+  a.blks = int(ceil_div(s.per, 16));
+  a.run_segs = s.segs - 1, a.run_first = BACK ? 1 : 0;
+  const int64_t wgs = int64_t(p.N) * p.G * a.blks * a.run_segs;
+  if (wgs * 256 > kMaxThreads) return CONV_ERANGE;
+  return p.S <= 32 ? ends_steps<T, 16, BACK>(p, s, a, wgs, st) : ends_steps<T, 8, BACK>(p, s, a, wgs, st);
+}
+
+template <typename T, int RW, int TS>
+int fwd_pass(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
+  constexpr int pass = 64 / RW * TS, per = pass / kChunk;
+  const int64_t lds = ((4 * p.S + 1) * int64_t(pass) + s.waves * (1 + per) * RW * ((p.S + 1) & ~1)) * 4;
+  // (512 steps of 32 rows by 4 waves; else 256 of 32 or 128 of 64 by 4, 128 of 128 by 8)
+  return with_loads<RW == 1 ? 8 : 4>(2 * p.S, pass, s.waves, [&](auto nb) {
+    return launch(scan_fwd_kernel<T, RW, TS, decltype(nb)::value>, s.wgs, s.waves * 64, lds, st, a);
+  });
 }
 template <typename T>
 int fwd(const seq_scan_t& p, hipStream_t st) {
@@ -983,31 +1074,22 @@ int fwd(const seq_scan_t& p, hipStream_t st) {
   a.ends = static_cast<float*>(p.workspace);
   a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * p.D * p.S);
   if (s.segs > 1) {
-    const int rc = fwd_kind<T, true>(p, s, a, st);
+    const int rc = ends_pass<T, false>(p, s, a, st);
     if (rc != CONV_OK) return rc;
   }
-  return fwd_kind<T, false>(p, s, a, st);
+  if (s.rows == 1) return fwd_pass<T, 1, 8>(p, s, a, st);
+  return s.steps == 16 ? fwd_pass<T, 4, 16>(p, s, a, st) : fwd_pass<T, 4, 8>(p, s, a, st);
 }
 
 // As many as LDS holds beside what S states need: an exchange is two barriers.
 int batch_of(int S) { return S > 32 ? 4 : S > 16 || S <= 8 ? 8 : 16; }
-template <typename T, bool GATE, bool ENDS>
-int bwd_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st) {
-  a.run_segs = ENDS ? s.segs - 1 : s.segs, a.run_first = ENDS ? 1 : 0;
-  const int rows = ENDS ? p.S : 2 * p.S, Se = (p.S + 1) & ~1;
-  const int64_t lds =
-      ((rows + 1) * int64_t(kChunk) + (ENDS ? 0 : a.batch * s.waves * 256) + s.waves * (ENDS ? 8 : 16) * Se) * 4;
-  return with_loads<ENDS ? 4 : 8>(rows, kChunk, s.waves, [&](auto nb) {
-    return launch(scan_bwd_kernel<T, decltype(nb)::value, GATE, ENDS>, s.wgs / s.segs * a.run_segs, s.waves * 64, lds, st, a);
-  });
-}
 template <typename T, bool GATE>
-int bwd_passes(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
-  if (s.segs > 1) {
-    const int rc = bwd_pass<T, GATE, true>(p, s, a, st);
-    if (rc != CONV_OK) return rc;
-  }
-  return bwd_pass<T, GATE, false>(p, s, a, st);
+int bwd_pass(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
+  const int rows = 2 * p.S, Se = (p.S + 1) & ~1;
+  const int64_t lds = ((rows + 1) * int64_t(kChunk) + a.batch * s.waves * 256 + s.waves * 16 * Se) * 4;
+  return with_loads<8>(rows, kChunk, s.waves, [&](auto nb) {
+    return launch(scan_bwd_kernel<T, decltype(nb)::value, GATE>, s.wgs, s.waves * 64, lds, st, a);
+  });
 }
 template <typename T>
 int bwd(const seq_scan_t& p, hipStream_t st) {
@@ -1024,7 +1106,8 @@ int bwd(const seq_scan_t& p, hipStream_t st) {
   a.part_D = a.part_A + pad4(int64_t(p.N) * s.segs * p.D * p.S);
   a.ends = a.part_D + pad4(int64_t(p.N) * s.segs * p.D * 2);
   a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * p.D * p.S);
-  const int rc = p.z ? bwd_passes<T, true>(p, s, a, st) : bwd_passes<T, false>(p, s, a, st);
+  int rc = s.segs > 1 ? ends_pass<T, true>(p, s, a, st) : CONV_OK;
+  if (rc == CONV_OK) rc = p.z ? bwd_pass<T, true>(p, s, a, st) : bwd_pass<T, false>(p, s, a, st);
   if (rc != CONV_OK) return rc;
   scan_sum_kernel<T><<<dim3(uint32_t(sum_wgs)), 256, 0, st>>>(a, uint32_t(bc_wgs));
   return hipGetLastError() == hipSuccess ? CONV_OK : CONV_EHIP;
