@@ -20,7 +20,7 @@
 //
 // Forward, bf16, 4 x 2048 x 2048 with 16 states and gate (2^28 steps of states):
 // 80 us, 10.4 issue slots a step of a state (7 of them the recurrence itself),
-// slots in use 82% of the time.  1 x 1024 x 16384 (2^28 too, cut into 8): 150 us.
+// slots in use 82% of the time.  1 x 1024 x 16384 (2^28 too, cut into 8): 145 us.
 #include <type_traits>
 
 #include "seq_device.h"
@@ -49,7 +49,8 @@ struct ScanArgs {
   T *du, *ddelta, *dz, *dB, *dC;
   float *dA, *dD, *dbias, *dinitial;
   // scratch
-  float *ends, *end_dt;    // [N][segs][D][S], [N][segs][D]
+  int fine, fine_chunks;   // pieces of a segment whose ends are found; their chunks
+  float *ends, *end_dt;    // [N][segs * fine][D][S], [N][segs * fine][D]
   float* part_bc;          // [N][G][blks][S][2][chunks * 128], a chunk's steps as in LDS
   float *part_A, *part_D;  // [N][segs][D][S], [N][segs][D][2] (Dskip, delta_bias)
 };
@@ -167,12 +168,12 @@ __device__ __forceinline__ float row_sum(float v) {
   return v;
 }
 
-// h (or a gradient) as the segments [from, to) in turn leave it; `at` is the
-// state's place in a segment's `ends`, d its channel.
+// h (or a gradient) as the pieces of segments from `from` to before `to` in turn
+// leave it; `at` is the state's place in a piece's `ends`, d its channel.
 template <typename T>
 __device__ __forceinline__ float through(const ScanArgs<T>& a, int n, int from, int to, int step, int64_t at, int d,
                                          float A2, float h) {
-  const int64_t first = int64_t(n) * a.segs + from;
+  const int64_t first = int64_t(n) * a.segs * a.fine + from;
   const float *dt = a.end_dt + first * a.D + d, *end = a.ends + first * a.D * a.S + at;
   const int64_t dt_step = int64_t(step) * a.D, end_step = dt_step * a.S;
 #pragma unroll 4
@@ -234,7 +235,7 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
       const int64_t at = state_at(a, p, 0) + int64_t(r) * S + s;
       A2 = kLog2e * a.A[at];
       if (a.initial) h = a.initial[int64_t(p.n) * a.D * S + at];
-      if (p.seg) h = through(a, p.n, 0, p.seg, 1, at, p.d0 + r, A2, h);
+      if (p.seg) h = through(a, p.n, 0, p.seg * a.fine, 1, at, p.d0 + r, A2, h);
     }
     as[e] = A2;
     hs[e] = h;
@@ -365,13 +366,14 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
   }
 }
 
-// What a segment alone makes of a zero state, and its sum of dt: forward, h at
+// What a piece of a segment alone makes of a zero state, and its sum of dt: forward, h at
 // its right end, the sum of x(t) B(t) exp(A (dt behind t)); BACK, r at its left
 // end, the sum of dy(t) C(t) exp(A (dt up to and with t)).  The steps stand side
 // by side, weighted with their decay to that end, so a state needs no scan, only
 // a sum over the row; the decays' exponents are sums of dt, taken along as the
-// passes walk away from the end.  1 x 1024 x 16384, 16 states, seven segments of
-// eight: ENDS_US us.
+// passes walk away from the end.  A segment is cut further (`fine`), for more waves
+// than the scan's registers allow: 1 x 1024 x 16384, 16 states, seven segments of
+// eight, 63 us whole and 59 in two pieces each.
 template <typename T, int TS, int NB, bool BACK>
 __global__ __launch_bounds__(512) void scan_ends_kernel(const ScanArgs<T> a) {
   extern __shared__ float lds[];
@@ -379,8 +381,11 @@ __global__ __launch_bounds__(512) void scan_ends_kernel(const ScanArgs<T> a) {
   const Place p = place<4>(a);
   const int S = a.S, Se = (S + 1) & ~1, lane = p.lane, row = p.row, tl = p.tl;
   const int len = seq_len(a.lengths, p.n, a.L);
-  const int first = p.seg * a.seg_chunks * kChunk;
-  const int stop = p.seg == a.segs - 1 ? a.L : first + a.seg_chunks * kChunk, end = len < stop ? len : stop;
+  const int seg = p.seg / a.fine, piece = p.seg - seg * a.fine;  // (p.seg: of the pieces)
+  const int c0 = seg * a.seg_chunks + piece * a.fine_chunks;
+  const int cs = seg == a.segs - 1 ? a.chunks : (seg + 1) * a.seg_chunks, c1 = c0 + a.fine_chunks < cs ? c0 + a.fine_chunks : cs;
+  const int64_t stop64 = int64_t(c1) * kChunk;
+  const int first = c0 * kChunk, end = len < stop64 ? len : int(stop64);
   const int passes = end > first ? (end - first + kSteps - 1) / kSteps : 0;
   float* bc = lds;  // [2][S], a row of zeros behind them
   float* zeros = bc + 2 * S * kSteps;
@@ -480,7 +485,7 @@ __global__ __launch_bounds__(512) void scan_ends_kernel(const ScanArgs<T> a) {
     if (k + 1 < passes) st.store(bc + ((k + 1) & 1) * S * kSteps, S);
     __syncthreads();
   }
-  const int64_t at = int64_t(p.n) * a.segs + p.seg;
+  const int64_t at = int64_t(p.n) * a.segs * a.fine + p.seg;
   float* to = a.ends + state_at(a, p, at);
   for (int e = lane; e < p.held * S; e += 64) to[e] = hs[e + e / S * (Se - S)];
   if (tl == 0 && p.ok) a.end_dt[at * a.D + p.d] = total;
@@ -544,7 +549,7 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
       const int64_t at = state_at(a, p, 0) + int64_t(r0) * S + s;
       A2 = kLog2e * a.A[at];
       if (a.dfinal) r = a.dfinal[int64_t(p.n) * a.D * S + at];
-      if (p.seg < a.segs - 1) r = through(a, p.n, a.segs - 1, p.seg, -1, at, p.d0 + r0, A2, r);
+      if (p.seg < a.segs - 1) r = through(a, p.n, a.segs * a.fine - 1, (p.seg + 1) * a.fine - 1, -1, at, p.d0 + r0, A2, r);
     }
     as[e] = A2;
     rs[e] = r;
@@ -955,6 +960,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
 struct Shape {
   int per, rows, waves, blks, segs, seg_chunks, chunks;  // rows: channels of a wave
   int steps;  // a lane's in a pass
+  int fine, fine_chunks;
   int64_t wgs;
 };
 Shape shape_of(const seq_scan_t& p, bool bwd) {
@@ -970,7 +976,7 @@ Shape shape_of(const seq_scan_t& p, bool bwd) {
   } else {
     // Few and short rows: a channel has a whole wave, 512 steps a pass (which
     // fits in LDS for up to 16 states).  2 x 520 x 1001: 15 us, against 22 in
-    // segments; 1 x 1024 x 16384: 176 us, against 148.
+    // segments; 1 x 1024 x 16384: 176 us, against 145.
     if (waves4 <= 1024 && p.L > 256 && p.L <= 2048 && p.S <= 16) s.rows = 1;
     s.waves = p.S > 32 ? 8 : 4;
   }
@@ -993,18 +999,23 @@ Shape shape_of(const seq_scan_t& p, bool bwd) {
   s.seg_chunks = int(ceil_div(passes, want)) * per;
   s.segs = int(ceil_div(s.chunks, s.seg_chunks));
   s.wgs = wgs * s.segs;
+  // (pieces of 256 steps at least, 4096 waves)
+  s.fine = 1;
+  while (s.fine < 4 && waves4 * (s.segs - 1) * s.fine < 3072 && s.seg_chunks >= 4 * s.fine) s.fine *= 2;
+  s.fine_chunks = int(ceil_div(s.seg_chunks, s.fine));
   return s;
 }
 int64_t pad4(int64_t n) { return (n + 3) / 4 * 4; }
 int64_t ends_floats(const seq_scan_t& p, const Shape& s) {
-  return s.segs > 1 ? pad4(int64_t(p.N) * s.segs * p.D * p.S) + pad4(int64_t(p.N) * s.segs * p.D) : 0;
+  const int64_t pieces = int64_t(p.N) * s.segs * s.fine;
+  return s.segs > 1 ? pad4(pieces * p.D * p.S) + pad4(pieces * p.D) : 0;
 }
 
 template <typename T>
 ScanArgs<T> args_of(const seq_scan_t& p, const Shape& s) {
   ScanArgs<T> a = {};
   a.N = p.N, a.D = p.D, a.L = p.L, a.S = p.S, a.G = p.G, a.per = s.per, a.softplus = p.delta_softplus;
-  a.blks = s.blks, a.segs = a.run_segs = s.segs, a.seg_chunks = s.seg_chunks, a.chunks = s.chunks;
+  a.blks = s.blks, a.segs = a.run_segs = s.segs, a.fine = s.fine, a.fine_chunks = s.fine_chunks, a.seg_chunks = s.seg_chunks, a.chunks = s.chunks;
   a.u_n = p.u_n, a.u_d = p.u_d, a.delta_n = p.delta_n, a.delta_d = p.delta_d, a.z_n = p.z_n, a.z_d = p.z_d;
   a.dout_n = p.dout_n, a.dout_d = p.dout_d;
   a.B_n = p.B_n, a.B_g = p.B_g, a.B_s = p.B_s, a.C_n = p.C_n, a.C_g = p.C_g, a.C_s = p.C_s;
@@ -1049,7 +1060,7 @@ int ends_steps(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, int64_
 template <typename T, bool BACK>
 int ends_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st) {
   a.blks = int(ceil_div(s.per, 16));
-  a.run_segs = s.segs - 1, a.run_first = BACK ? 1 : 0;
+  a.run_segs = (s.segs - 1) * s.fine, a.run_first = BACK ? s.fine : 0;
   const int64_t wgs = int64_t(p.N) * p.G * a.blks * a.run_segs;
   if (wgs * 256 > kMaxThreads) return CONV_ERANGE;
   return p.S <= 32 ? ends_steps<T, 16, BACK>(p, s, a, wgs, st) : ends_steps<T, 8, BACK>(p, s, a, wgs, st);
@@ -1072,7 +1083,7 @@ int fwd(const seq_scan_t& p, hipStream_t st) {
   if (s.segs > 1 && p.workspace_bytes < scan_fwd_workspace(p)) return CONV_ESCRATCH;
   ScanArgs<T> a = args_of<T>(p, s);
   a.ends = static_cast<float*>(p.workspace);
-  a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * p.D * p.S);
+  a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * s.fine * p.D * p.S);
   if (s.segs > 1) {
     const int rc = ends_pass<T, false>(p, s, a, st);
     if (rc != CONV_OK) return rc;
@@ -1105,7 +1116,7 @@ int bwd(const seq_scan_t& p, hipStream_t st) {
   a.part_A = a.part_bc + int64_t(p.N) * p.G * s.blks * p.S * 2 * s.chunks * kChunk;
   a.part_D = a.part_A + pad4(int64_t(p.N) * s.segs * p.D * p.S);
   a.ends = a.part_D + pad4(int64_t(p.N) * s.segs * p.D * 2);
-  a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * p.D * p.S);
+  a.end_dt = a.ends + pad4(int64_t(p.N) * s.segs * s.fine * p.D * p.S);
   int rc = s.segs > 1 ? ends_pass<T, true>(p, s, a, st) : CONV_OK;
   if (rc == CONV_OK) rc = p.z ? bwd_pass<T, true>(p, s, a, st) : bwd_pass<T, false>(p, s, a, st);
   if (rc != CONV_OK) return rc;
