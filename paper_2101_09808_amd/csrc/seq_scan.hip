@@ -999,9 +999,9 @@ Shape shape_of(const seq_scan_t& p, bool bwd) {
   s.seg_chunks = int(ceil_div(passes, want)) * per;
   s.segs = int(ceil_div(s.chunks, s.seg_chunks));
   s.wgs = wgs * s.segs;
-  // (pieces of 256 steps at least, 4096 waves)
+  // (pieces of 256 steps at least, up to 4096 waves of them)
   s.fine = 1;
-  while (s.fine < 4 && waves4 * (s.segs - 1) * s.fine < 3072 && s.seg_chunks >= 4 * s.fine) s.fine *= 2;
+  while (s.fine < 4 && waves4 * (s.segs - 1) * s.fine * 2 <= 4096 && s.seg_chunks >= 4 * s.fine) s.fine *= 2;
   s.fine_chunks = int(ceil_div(s.seg_chunks, s.fine));
   return s;
 }
