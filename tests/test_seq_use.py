@@ -328,7 +328,7 @@ def test_inputs_past_32_bit_offsets():
 
 def test_outputs_past_32_bit_offsets():
     """2^31 elements and more in one call: its last rows are those of a call of their own."""
-    D, L = 70000, 30720
+    D, L = 70000, 30688
     x = torch.empty((1, D, L), dtype=BF, device=DEV)
     G = Gen(20)
     tail = G.n(1, 3, L, dtype=BF)
