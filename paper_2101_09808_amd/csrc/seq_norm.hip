@@ -208,15 +208,15 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
       g[k] = has_g ? cols<IN, T>(gp, dc, a.gate_d, nv) : Raw8<T>{};
       r[k] = !POST && has_r ? cols<IN, R>(rp, dc, a.res_d, nv) : Raw8<R>{};
     }
+    float held[H][8];
 #pragma unroll
     for (int k = 0; k < H; ++k) {
       const int d = d0 + k * RS;
-      if (PHASE != kRest && d < rows) {
-        float v[8];
-        terms(x[k], g[k], r[k], d, v);
-        first(v, d);
+      if (d < rows) {
+        terms(x[k], g[k], r[k], d, held[k]);
+        if (PHASE != kRest) first(held[k], d);
       }
-      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_sched_barrier(0);  // (one channel's registers at a time)
     }
     auto again_at = [&](int d, float* v, Raw8<R>& rr) {
       const Raw8<T> xx = cols<IN, T>(xp, d, a.x_d, nv), gg = has_g ? cols<IN, T>(gp, d, a.gate_d, nv) : Raw8<T>{};
@@ -250,12 +250,8 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
 #pragma unroll
     for (int k = 0; k < H; ++k) {
       const int d = d0 + k * RS;
-      if (d < rows) {
-        float v[8];
-        terms(again(x[k]), again(g[k]), POST ? r[k] : again(r[k]), d, v);
-        second(v, r[k], d);
-      }
-      __builtin_amdgcn_sched_barrier(0);  // (one channel's registers at a time)
+      if (d < rows) second(held[k], r[k], d);
+      __builtin_amdgcn_sched_barrier(0);
     }
     for (int d = d0 + H * RS; d < rows; d += RS) {
       float v[8];
