@@ -229,6 +229,15 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
       again_at(d, v, rr);
       first(v, d);
     }
+    // (after a block: the residual, on its way while the sums are formed)
+    if (POST && PHASE != kSums) {
+      d0 = fresh(d0);
+#pragma unroll
+      for (int k = 0; k < H; ++k) {
+        const int d = d0 + k * RS;
+        r[k] = has_r ? cols<IN, R>(rp, d < rows ? d : rows - 1, a.res_d, nv) : Raw8<R>{};
+      }
+    }
     if (PHASE == kRest)
       sums.take(stats, a.parts, s);
     else
@@ -240,13 +249,6 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
     d0 = fresh(d0);
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[0][j] = __builtin_amdgcn_rsqf(__builtin_fmaf(s[0][j], a.inv_d, a.eps));
-    if (POST) {
-#pragma unroll
-      for (int k = 0; k < H; ++k) {
-        const int d = d0 + k * RS;
-        r[k] = has_r ? cols<IN, R>(rp, d < rows ? d : rows - 1, a.res_d, nv) : Raw8<R>{};
-      }
-    }
 #pragma unroll
     for (int k = 0; k < H; ++k) {
       const int d = d0 + k * RS;
