@@ -640,7 +640,7 @@ Shape shape_of(const seq_norm_t& p) {
     // Whole channels at once where each CU has a tile of at least 32 columns
     // (whole cache lines of bf16) and half of its channels stay in registers;
     // else cut.  Forward and backward, whole (at CL 2 or 4) and cut (at 8):
-    // bf16 4 x 2048 x 2048 105 and 105 us, fp32 3 x 1000 x 1333 66 and 59,
+    // bf16 4 x 2048 x 2048 98 and 105 us, fp32 3 x 1000 x 1333 66 and 59,
     // bf16 9 x 2816 x 53 110 and 45.
     tile(p.L > 32 ? 8 : p.L > 16 ? 4 : 2);
     const auto whole = [&] { return s.tiles >= 256 && int64_t(p.D) * s.cl <= 8192; };
