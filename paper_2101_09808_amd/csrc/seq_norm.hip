@@ -11,9 +11,12 @@
 // The length is innermost, so a column's channels lie L apart: a workgroup
 // takes all channels of a tile of 8 CL columns, CL lanes of eight columns a
 // channel, and goes over it twice (statistics, results).  The first H channels
-// of a thread stay in registers between the two, as they were loaded; what is
-// more is read again.  Loads go out before anything waits for them: a tile that
-// lies whole inside the row has no conditions on the way.
+// of a thread stay in registers between the two (forward what is normed,
+// backward what was loaded); what is more is read again.  Loads go out before
+// anything waits for them: a tile that lies whole inside the row has no
+// conditions on the way.  bf16 4 x 2048 x 2048 with gate and residual: forward 43
+// us (134 MB, 3.1 TB/s), backward 50 (168 MB, 3.4 TB/s); a CU has one workgroup,
+// whose reading, sums and writing follow one another.
 #include <type_traits>
 
 #include "seq_device.h"
