@@ -11,7 +11,7 @@
 
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/core/Tensor.h>
-#include <ATen/ops/empty.h>
+#include <ATen/ops/empty_cuda_dispatch.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -108,7 +108,9 @@ struct Call {
     return o == Py_None ? nullptr : static_cast<P*>(dense(o, name, sizes, t).data_ptr());
   }
   Tensor empty(IntArrayRef sizes, ScalarType t) const {
-    return at::empty(sizes, at::TensorOptions().dtype(t).device(like.device()));
+    // (at::empty without its way through the dispatcher: a backward scan has ten
+    // results)
+    return at::cuda::empty(sizes, at::TensorOptions().dtype(t).device(like.device()));
   }
   Tensor out(PyObject* o, IntArrayRef sizes, ScalarType t) const {
     return o == Py_None ? empty(sizes, t) : dense(o, "out", sizes, t);
