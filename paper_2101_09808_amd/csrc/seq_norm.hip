@@ -151,7 +151,8 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const NormArgs a) {
   using Out = typename NormTypes<T, R, POST>::Out;
   __shared__ ColumnSums<NT, CL, 1> sums;
   constexpr int RS = NT / CL;
-  const uint32_t part = PHASE ? blockIdx.x % a.parts : 0, tile = PHASE ? blockIdx.x / a.parts : tile_of(blockIdx.x, a.tiles);
+  const uint32_t part = PHASE ? blockIdx.x % a.parts : 0;
+  const uint32_t tile = PHASE ? blockIdx.x / a.parts : tile_of(blockIdx.x, a.tiles);
   const int rows = PHASE && int(part + 1) * a.part < a.D ? int(part + 1) * a.part : a.D;  // (the part's end)
   float* const stats = PHASE ? a.stats + (int64_t(tile) * a.parts + (PHASE == kSums ? part : 0)) * (CL * 8) : nullptr;
   const int n = int(tile / a.row_tiles);

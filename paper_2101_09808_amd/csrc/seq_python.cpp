@@ -2,7 +2,7 @@
 // wraps): checks torch tensors against each other, allocates results and
 // scratch from torch's allocator and makes the C ABI's call on the current
 // stream of the tensors' device.  A call of the smallest sizes takes the GPU 3
-// us; through ctypes its marshalling took the host 11 to 17, here about 5.
+// us; through ctypes its marshalling took the host 11 to 17, here 4 to 5.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -250,7 +250,8 @@ seq_scan_t scan_args(const Call& c, const Tensor& u, PyObject* delta, PyObject* 
   if (Bt.dim() != u.dim() + 1)
     value_error(std::string("B must be [N, G, S") + (many ? ", L]" : "]") + ", got " + text(Bt.sizes()));
   const int64_t G = Bt.size(1);
-  if (G < 1 || Dn % G) value_error(std::to_string(Dn) + " channels do not divide into " + std::to_string(G) + " groups");
+  if (G < 1 || Dn % G)
+    value_error(std::to_string(Dn) + " channels do not divide into " + std::to_string(G) + " groups");
   const int64_t L = many ? u.size(2) : 1, bs[4] = {N, G, S, L};
   const IntArrayRef bsize(bs, many ? 4 : 3);
   const auto get = [&](PyObject* o, const char* name, IntArrayRef sizes) -> const Tensor& {

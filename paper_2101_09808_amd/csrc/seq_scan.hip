@@ -383,7 +383,8 @@ __global__ __launch_bounds__(512) void scan_ends_kernel(const ScanArgs<T> a) {
   const int len = seq_len(a.lengths, p.n, a.L);
   const int seg = p.seg / a.fine, piece = p.seg - seg * a.fine;  // (p.seg: of the pieces)
   const int c0 = seg * a.seg_chunks + piece * a.fine_chunks;
-  const int cs = seg == a.segs - 1 ? a.chunks : (seg + 1) * a.seg_chunks, c1 = c0 + a.fine_chunks < cs ? c0 + a.fine_chunks : cs;
+  const int cs = seg == a.segs - 1 ? a.chunks : (seg + 1) * a.seg_chunks;
+  const int c1 = c0 + a.fine_chunks < cs ? c0 + a.fine_chunks : cs;
   const int64_t stop64 = int64_t(c1) * kChunk;
   const int first = c0 * kChunk, end = len < stop64 ? len : int(stop64);
   const int passes = end > first ? (end - first + kSteps - 1) / kSteps : 0;
@@ -549,7 +550,8 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
       const int64_t at = state_at(a, p, 0) + int64_t(r0) * S + s;
       A2 = kLog2e * a.A[at];
       if (a.dfinal) r = a.dfinal[int64_t(p.n) * a.D * S + at];
-      if (p.seg < a.segs - 1) r = through(a, p.n, a.segs * a.fine - 1, (p.seg + 1) * a.fine - 1, -1, at, p.d0 + r0, A2, r);
+      if (p.seg < a.segs - 1)
+        r = through(a, p.n, a.segs * a.fine - 1, (p.seg + 1) * a.fine - 1, -1, at, p.d0 + r0, A2, r);
     }
     as[e] = A2;
     rs[e] = r;
@@ -792,7 +794,8 @@ __global__ __launch_bounds__(256) void scan_sum_kernel(const ScanArgs<T> a, uint
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (c * kChunk < len) {
       const int64_t step = int64_t(a.S) * 2 * a.chunks * kChunk;
-      const float* from = a.part_bc + ng * a.blks * step + (int64_t(s) * 2 + which) * a.chunks * kChunk + int64_t(q) * 4;
+      const float* from =
+          a.part_bc + ng * a.blks * step + (int64_t(s) * 2 + which) * a.chunks * kChunk + int64_t(q) * 4;
 #pragma unroll 16
       for (int b = 0; b < a.blks; ++b) v += *reinterpret_cast<const f32x4*>(from + b * step);
     }
@@ -1015,7 +1018,8 @@ template <typename T>
 ScanArgs<T> args_of(const seq_scan_t& p, const Shape& s) {
   ScanArgs<T> a = {};
   a.N = p.N, a.D = p.D, a.L = p.L, a.S = p.S, a.G = p.G, a.per = s.per, a.softplus = p.delta_softplus;
-  a.blks = s.blks, a.segs = a.run_segs = s.segs, a.fine = s.fine, a.fine_chunks = s.fine_chunks, a.seg_chunks = s.seg_chunks, a.chunks = s.chunks;
+  a.blks = s.blks, a.segs = a.run_segs = s.segs, a.seg_chunks = s.seg_chunks, a.chunks = s.chunks;
+  a.fine = s.fine, a.fine_chunks = s.fine_chunks;
   a.u_n = p.u_n, a.u_d = p.u_d, a.delta_n = p.delta_n, a.delta_d = p.delta_d, a.z_n = p.z_n, a.z_d = p.z_d;
   a.dout_n = p.dout_n, a.dout_d = p.dout_d;
   a.B_n = p.B_n, a.B_g = p.B_g, a.B_s = p.B_s, a.C_n = p.C_n, a.C_g = p.C_g, a.C_s = p.C_s;

@@ -47,19 +47,16 @@ def native():
     return _native
 
 
-def _call(name, args, stream):
-    f = getattr(_native or native(), name)
-    if stream is None:
-        return f(*args)
-    # Results are allocated on the stream; tensors of another stream's pool are
-    # recorded on it, so that freeing them does not hand their memory on while
-    # the call still runs.
-    tensors = [t for t in args if isinstance(t, torch.Tensor) and t.is_cuda]
-    for t in tensors:
-        if t.device != stream.device:
-            raise ValueError(f"stream is on {stream.device}, a tensor is on {t.device}")
-        if stream != torch.cuda.current_stream(t.device):
-            t.record_stream(stream)
+def _on(stream, f, *args):
+    """f(*args) on `stream`.  Results are allocated on it; tensors of another
+    stream's pool are recorded on it, so that freeing them does not hand their
+    memory on while the call still runs."""
+    for t in args:
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            if t.device != stream.device:
+                raise ValueError(f"stream is on {stream.device}, a tensor is on {t.device}")
+            if stream != torch.cuda.current_stream(t.device):
+                t.record_stream(stream)
     with torch.cuda.stream(stream):
         return f(*args)
 
@@ -114,8 +111,9 @@ def causal_conv_fwd(x, weight, bias=None, *, activation=None, initial_state=None
     ``return_final_state``: the last R-1 entries of each sequence, the
     ``initial_state`` of the call that continues it.
     """
-    return _call("causal_conv_fwd",
-                 (x, weight, bias, activation, initial_state, lengths, return_final_state, out), stream)
+    f = (_native or native()).causal_conv_fwd
+    args = (x, weight, bias, activation, initial_state, lengths, return_final_state, out)
+    return f(*args) if stream is None else _on(stream, f, *args)
 
 
 def causal_conv_bwd(dout, x, weight, bias=None, *, activation=None, initial_state=None, lengths=None,
@@ -124,15 +122,18 @@ def causal_conv_bwd(dout, x, weight, bias=None, *, activation=None, initial_stat
     arguments, for ``dout`` ``[N, D, L]`` and, if the final state was used,
     ``dfinal_state``.  ``dbias`` and ``dinitial_state`` are None where the call
     had no bias or initial state."""
-    return ConvGrads(*_call("causal_conv_bwd",
-                            (dout, x, weight, bias, activation, initial_state, lengths, dfinal_state), stream))
+    f = (_native or native()).causal_conv_bwd
+    args = (dout, x, weight, bias, activation, initial_state, lengths, dfinal_state)
+    return ConvGrads(*(f(*args) if stream is None else _on(stream, f, *args)))
 
 
 def causal_conv_step(x, state, weight, bias=None, *, activation=None, new_state=None, out=None, stream=None):
     """One token of :func:`causal_conv_fwd`: x ``[N, D]`` (any strides), state
     ``[N, D, R-1]``.  Returns out ``[N, D]``; the state after the token goes to
     ``new_state``, by default in place of ``state``."""
-    return _call("causal_conv_step", (x, state, weight, bias, activation, new_state, out), stream)
+    f = (_native or native()).causal_conv_step
+    args = (x, state, weight, bias, activation, new_state, out)
+    return f(*args) if stream is None else _on(stream, f, *args)
 
 
 # -------------------------------------------------------------- selective scan
@@ -154,9 +155,10 @@ def selective_scan_fwd(u, delta, A, B, C, *, D=None, z=None, delta_bias=None, de
     ``checkpoints`` (with ``return_checkpoints``; the state before every 128th
     step), in this order.
     """
-    return _call("selective_scan_fwd",
-                 (u, delta, A, B, C, D, z, delta_bias, delta_softplus, initial_state, lengths, return_final_state,
-                  return_checkpoints, out), stream)
+    f = (_native or native()).selective_scan_fwd
+    args = (u, delta, A, B, C, D, z, delta_bias, delta_softplus, initial_state, lengths, return_final_state,
+            return_checkpoints, out)
+    return f(*args) if stream is None else _on(stream, f, *args)
 
 
 def selective_scan_bwd(dout, u, delta, A, B, C, checkpoints, *, D=None, z=None, delta_bias=None,
@@ -165,9 +167,9 @@ def selective_scan_bwd(dout, u, delta, A, B, C, checkpoints, *, D=None, z=None, 
     arguments, from the ``checkpoints`` that it returned.  Gradients of
     arguments that the call did not have are None; ``dinitial_state`` is always
     formed."""
-    return ScanGrads(*_call("selective_scan_bwd",
-                            (dout, u, delta, A, B, C, checkpoints, D, z, delta_bias, delta_softplus, lengths,
-                             dfinal_state), stream))
+    f = (_native or native()).selective_scan_bwd
+    args = (dout, u, delta, A, B, C, checkpoints, D, z, delta_bias, delta_softplus, lengths, dfinal_state)
+    return ScanGrads(*(f(*args) if stream is None else _on(stream, f, *args)))
 
 
 def selective_scan_step(u, state, delta, A, B, C, *, D=None, z=None, delta_bias=None, delta_softplus=False,
@@ -176,8 +178,9 @@ def selective_scan_step(u, state, delta, A, B, C, *, D=None, z=None, delta_bias=
     ``[N, G, S]`` (any strides), state ``[N, D, S]`` fp32.  Returns out
     ``[N, D]``; the state after the token goes to ``new_state``, by default in
     place of ``state``."""
-    return _call("selective_scan_step",
-                 (u, state, delta, A, B, C, D, z, delta_bias, delta_softplus, new_state, out), stream)
+    f = (_native or native()).selective_scan_step
+    args = (u, state, delta, A, B, C, D, z, delta_bias, delta_softplus, new_state, out)
+    return f(*args) if stream is None else _on(stream, f, *args)
 
 
 # ------------------------------------------------------------------------ norms
@@ -188,14 +191,18 @@ def norm_pre_fwd(x, weight, *, residual=None, scale=None, eps=1e-6, out=None, st
     channels of each position.  x, residual ``[N, D, L]`` (residual of x's type
     or fp32), weight and scale ``[D]`` fp32.  Returns (out of x's type, sum of
     the residual's); without a residual ``sum`` is ``scale x``."""
-    return _call("norm_pre_fwd", (x, weight, residual, scale, eps, out), stream)
+    f = (_native or native()).norm_pre_fwd
+    args = (x, weight, residual, scale, eps, out)
+    return f(*args) if stream is None else _on(stream, f, *args)
 
 
 def norm_pre_bwd(dout, sum, weight, *, dsum=None, x=None, scale=None, eps=1e-6, stream=None):
     """:class:`NormPreGrads` of :func:`norm_pre_fwd` from the ``sum`` that it
     returned; ``dsum`` is the gradient that reaches ``sum`` from elsewhere (the
     residual stream).  ``x`` is needed where the call had a ``scale``."""
-    return NormPreGrads(*_call("norm_pre_bwd", (dout, sum, weight, dsum, x, scale, eps), stream))
+    f = (_native or native()).norm_pre_bwd
+    args = (dout, sum, weight, dsum, x, scale, eps)
+    return NormPreGrads(*(f(*args) if stream is None else _on(stream, f, *args)))
 
 
 def norm_post_fwd(x, weight, *, gate=None, residual=None, scale=None, eps=1e-6, out=None, stream=None):
@@ -204,10 +211,14 @@ def norm_post_fwd(x, weight, *, gate=None, residual=None, scale=None, eps=1e-6, 
     rstd(v)`` over the channels of each position.  x, gate, residual
     ``[N, D, L]`` (residual of x's type or fp32), weight and scale ``[D]``
     fp32.  Returns out, of the residual's type."""
-    return _call("norm_post_fwd", (x, weight, gate, residual, scale, eps, out), stream)
+    f = (_native or native()).norm_post_fwd
+    args = (x, weight, gate, residual, scale, eps, out)
+    return f(*args) if stream is None else _on(stream, f, *args)
 
 
 def norm_post_bwd(dout, x, weight, *, gate=None, scale=None, eps=1e-6, stream=None):
     """:class:`NormPostGrads` of :func:`norm_post_fwd`, for ``dout`` of its
     output's type."""
-    return NormPostGrads(*_call("norm_post_bwd", (dout, x, weight, gate, scale, eps), stream))
+    f = (_native or native()).norm_post_bwd
+    args = (dout, x, weight, gate, scale, eps)
+    return NormPostGrads(*(f(*args) if stream is None else _on(stream, f, *args)))
