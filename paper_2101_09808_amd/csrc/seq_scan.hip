@@ -231,11 +231,11 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
   for (int e = lane; e < RW * Se; e += 64) {
     const int r = e / Se, s = e - r * Se;
     float A2 = 0.f, h = 0.f;
-    if (r < held && s < S) {
+    if (r < held) {
       const int64_t at = state_at(a, p, 0) + int64_t(r) * S + s;
-      A2 = kLog2e * a.A[at];
-      if (a.initial) h = a.initial[int64_t(p.n) * a.D * S + at];
-      if (p.seg) h = through(a, p.n, 0, p.seg * a.fine, 1, at, p.d0 + r, A2, h);
+      A2 = kLog2e * a.A[s < S ? at : at - 1];
+      if (s < S && a.initial) h = a.initial[int64_t(p.n) * a.D * S + at];
+      if (s < S && p.seg) h = through(a, p.n, 0, p.seg * a.fine, 1, at, p.d0 + r, A2, h);
     }
     as[e] = A2;
     hs[e] = h;
@@ -288,7 +288,8 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
     }
     if (zp) fetch(zp, t0, rz);
     for (int s = 0; s < S; s += 2) {
-      // (with S odd the last state's pair is of decay 1 and reads zeros)
+      // (with S odd the last state's pair has its decay and reads zeros: it is not
+      // finite only where that state is not)
       const bool two = s + 1 < S;
       const float *b0 = cur + s * kSteps, *b1 = two ? b0 + kSteps : zeros;
       float w[2][TS], b[2][TS], A2[2], in[2], H[2], P[2];
@@ -546,11 +547,11 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
   for (int e = lane; e < 4 * Se; e += 64) {
     const int r0 = e / Se, s = e - r0 * Se;
     float A2 = 0.f, r = 0.f;
-    if (r0 < held && s < S) {
+    if (r0 < held) {
       const int64_t at = state_at(a, p, 0) + int64_t(r0) * S + s;
-      A2 = kLog2e * a.A[at];
-      if (a.dfinal) r = a.dfinal[int64_t(p.n) * a.D * S + at];
-      if (p.seg < a.segs - 1)
+      A2 = kLog2e * a.A[s < S ? at : at - 1];
+      if (s < S && a.dfinal) r = a.dfinal[int64_t(p.n) * a.D * S + at];
+      if (s < S && p.seg < a.segs - 1)
         r = through(a, p.n, a.segs * a.fine - 1, (p.seg + 1) * a.fine - 1, -1, at, p.d0 + r0, A2, r);
     }
     as[e] = A2;
@@ -634,8 +635,8 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
     }
     __syncthreads();
     if (c > c0) fetch(c - 1);
-    // Two states at a time (with S odd the last one's pair is of decay 1 and
-    // reads zeros), `batch` between two exchanges.
+    // Two states at a time (with S odd the last one's pair has its decay and reads
+    // zeros), `batch` between two exchanges.
     for (int s = 0; s < S; s += 2) {
       const bool two = s + 1 < S;
       const float* b0 = bc + s * kChunk;
@@ -720,8 +721,7 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         od[j] = __builtin_fmaf(dx[j], u[j], kLn2 * ddt[j]);
-        // softplus's slope exp(v) / (1 + exp(v)) = exp(v - softplus(v))
-        if (a.softplus) od[j] *= exp2_fast(kLog2e * (raw[j] + bias - dt[j]));
+        if (a.softplus) od[j] *= sigmoid(raw[j] + bias);  // (of an infinite step: 1)
         o[j] = __builtin_fmaf(dx[j], dt[j], skip * dy[j]);
       }
       if (GATE) {

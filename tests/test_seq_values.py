@@ -1,0 +1,48 @@
+"""Values at the ends of fp32's range in the selective scan: what is finite in
+the definition stays finite and right."""
+import pytest
+import torch
+
+from oracle import seq as O
+from paper_2101_09808_amd import seq
+from tests.test_seq_ops import F32, Gen, check, say, scan_inputs, scan_tolerance
+
+pytestmark = pytest.mark.gpu
+
+NAMES = ("du", "ddelta", "dA", "dB", "dC", "dD", "ddelta_bias", "dz", "dinitial_state")
+
+
+def check_finite(name, got, ref, count, mag):
+    """`check` where the definition is finite; elsewhere neither is."""
+    fin = torch.isfinite(ref)
+    assert torch.equal(torch.isfinite(got.cpu()), fin), (name, (torch.isfinite(got.cpu()) != fin).nonzero()[:4].tolist())
+    zero = torch.zeros((), dtype=ref.dtype)
+    check(name, torch.where(fin.to(got.device), got, 0), torch.where(fin, ref, zero), count, torch.where(fin, mag, zero))
+
+
+@pytest.mark.parametrize("N,D,L,S", [(2, 6, 140, 1), (2, 6, 300, 5), (2, 6, 300, 16), (1, 70, 290, 17), (1, 5, 200, 33),
+                                     (1, 4, 2600, 3)])
+def test_infinite_step(N, D, L, S):
+    """A step of infinite length wipes its channel's states out: gradients of
+    earlier steps, and of the step itself but for what multiplies it, are finite."""
+    say("[gpu] infinite step", N, D, L, S)
+    G = Gen(31)
+    v = scan_inputs(G, N, D, L, S, 1, F32, True, True, True, True)
+    t = L // 2 + 3
+    v["delta"][0, 2, t] = float("inf")
+    do, df = G.n(N, D, L), G.n(N, D, S)
+    pos = [v[k] for k in ("u", "delta", "A", "B", "C")]
+    kw = dict(D=v["D"], z=v["z"], delta_bias=v["delta_bias"], delta_softplus=True)
+    out, fin, chk = seq.selective_scan_fwd(*pos, initial_state=v["initial_state"], return_final_state=True,
+                                           return_checkpoints=True, **kw)
+    args = (*pos, v["D"], v["z"], v["delta_bias"], True, v["initial_state"])
+    ref, rfin, _, _, bound, fbound = O.selective_scan(*args)
+    check_finite("out", out, ref, 1.0, bound)
+    check_finite("final_state", fin, rfin, 1.0, fbound)
+    g = seq.selective_scan_bwd(do, *pos, chk, dfinal_state=df, **kw)
+    rg = O.selective_scan_grads(do, *args, None, df)
+    mg = O.selective_scan_grads(do, *args, None, df, absolute=True)
+    assert torch.isfinite(rg[0][0, 2, :t]).all() and torch.isfinite(rg[1][0, 2, :t + 1]).all()
+    for name, got, r, m in zip(NAMES, g, rg, mg):
+        many = D if name in ("dB", "dC") else N * L / 16 if name in ("dA", "dD", "ddelta_bias") else 0
+        check_finite(name, got, r, scan_tolerance(L, S) + many, m)
