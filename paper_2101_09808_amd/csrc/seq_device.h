@@ -136,6 +136,14 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// v 2^x, also where 2^x is past fp32's range: zero stays zero, and what the product
+// has in range is right.  (Beyond 2^504 and 2^-504 no v but zero has.)
+__device__ __forceinline__ float times_exp2(float v, float x) {
+  x = x > 504.f ? 504.f : x < -504.f ? -504.f : x;  // (NaN: kept)
+  const float f = exp2_fast(0.25f * x);
+  return v * f * f * f * f;
+}
+
 // 1 / (1 + exp(-x)): one exp2 and one reciprocal, each good to an ulp; exp(-x)
 // overflows to infinity, its reciprocal to 0.
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + exp2_fast(-kLog2e * x)); }

@@ -123,8 +123,9 @@ __device__ __forceinline__ void lds_steps(const float* lds, int tl, float* v) {
 
 // The states that reach each lane, for two states at once: H (a lane's steps
 // from zero; lane 0 has its incoming state in them) and P (their decay) are
-// composed in levels of 1, 2, 4 and 8 lanes, then over two and four rows where
-// a channel has the whole wave.  A lane without a source is left as it is.  H
+// composed in levels of 1, 2, 4 and 8 lanes, then from row to row where a channel
+// has the whole wave.  (So P is of kChunk steps at most: decays that overflow over
+// more of them stay out.)  A lane without a source is left as it is.  H
 // becomes the state behind each lane, `in` the one before it (lane 0: kept).
 // Written as DPP operands, which the compiler makes moves of; a DPP source has
 // to be two instructions old, which the two chains are to one another.
@@ -148,9 +149,10 @@ __device__ __forceinline__ void scan_lanes(float* H, float* P, float* in) {
                  : SEQ_SCAN_OPERANDS);
   else
     asm volatile(SEQ_ROW_LEVELS("row_shr") SEQ_LEVEL(SEQ_ROW("row_shr", 8))
-                     SEQ_LEVEL("row_bcast:15 row_mask:0xa bank_mask:0xf")
-                         SEQ_DPP2("v_fmac_f32_dpp", 0, 1, "row_bcast:31 row_mask:0xc bank_mask:0xf")
-                             SEQ_SHIFT("wave_shr:1")
+                     SEQ_DPP2("v_fmac_f32_dpp", 0, 1, "row_bcast:15 row_mask:0x2 bank_mask:0xf")
+                         "s_nop 0\n" SEQ_DPP2("v_fmac_f32_dpp", 0, 1, "row_bcast:15 row_mask:0x4 bank_mask:0xf")
+                             "s_nop 0\n" SEQ_DPP2("v_fmac_f32_dpp", 0, 1, "row_bcast:15 row_mask:0x8 bank_mask:0xf")
+                                 SEQ_SHIFT("wave_shr:1")
                  : SEQ_SCAN_OPERANDS);
 }
 // The same from right to left (lane 15 keeps its `in`), rows of sixteen.
@@ -178,7 +180,7 @@ __device__ __forceinline__ float through(const ScanArgs<T>& a, int n, int from, 
   const int64_t dt_step = int64_t(step) * a.D, end_step = dt_step * a.S;
 #pragma unroll 4
   for (int k = from; k != to; k += step, dt += dt_step, end += end_step)
-    h = __builtin_fmaf(exp2_fast(A2 * *dt), h, *end);
+    h = times_exp2(h, A2 * *dt) + *end;
   return h;
 }
 
@@ -372,7 +374,9 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
 // end, the sum of dy(t) C(t) exp(A (dt up to and with t)).  The steps stand side
 // by side, weighted with their decay to that end, so a state needs no scan, only
 // a sum over the row; the decays' exponents are sums of dt, taken along as the
-// passes walk away from the end.  A segment is cut further (`fine`), for more waves
+// passes walk away from the end.  Where those decays may grow (some A is positive, or
+// without softplus a step negative) they are past fp32 over a piece when they are
+// not over kChunk steps, and go into each product without being formed.  A segment is cut further (`fine`), for more waves
 // than the scan's registers allow: 1 x 1024 x 16384, 16 states, seven segments of
 // eight, 63 us whole and 59 in two pieces each.
 template <typename T, int TS, int NB, bool BACK>
@@ -393,11 +397,15 @@ __global__ __launch_bounds__(512) void scan_ends_kernel(const ScanArgs<T> a) {
   float* zeros = bc + 2 * S * kSteps;
   float* hs = zeros + kSteps + p.wave * 8 * Se;
   float* as = hs + 4 * Se;
+  bool grow = false;  // (the wave's)
   for (int e = lane; e < 4 * Se; e += 64) {
     const int r = e / Se, s = e - r * Se;
-    as[e] = r < p.held && s < S ? kLog2e * a.A[state_at(a, p, 0) + int64_t(r) * S + s] : 0.f;
+    const float A2 = r < p.held && s < S ? kLog2e * a.A[state_at(a, p, 0) + int64_t(r) * S + s] : 0.f;
+    as[e] = A2;
     hs[e] = 0.f;
+    grow |= A2 > 0.f;
   }
+  grow = __any(grow);
   for (int e = threadIdx.x; e < kSteps; e += blockDim.x) zeros[e] = 0.f;
   const bool gate = BACK && a.z;
   const T* dp = a.delta + p.n * a.delta_n + p.d * a.delta_d + tl * TS;
@@ -444,6 +452,12 @@ __global__ __launch_bounds__(512) void scan_ends_kernel(const ScanArgs<T> a) {
 #pragma unroll
       for (int j = 0; j < TS; ++j) v[j] *= dt[j];
     }
+    if (!a.softplus && !grow) {
+      bool negative = false;
+#pragma unroll
+      for (int j = 0; j < TS; ++j) negative |= dt[j] < 0.f;
+      grow = __any(negative);
+    }
     if (k + 1 < passes) fetch(at_pass(k + 1));
     // dt becomes each step's distance from the end: the lanes' sums first
     float lanes = sum;
@@ -471,18 +485,30 @@ __global__ __launch_bounds__(512) void scan_ends_kernel(const ScanArgs<T> a) {
         far += own;
       }
     }
-    for (int s = 0; s < S; s += 2) {
-      const float *m0 = cur + s * kSteps, *m1 = s + 1 < S ? m0 + kSteps : zeros;
-      float m[2][TS], H[2] = {0.f, 0.f};
-      const float A2[2] = {as[row * Se + s], as[row * Se + s + 1]};
-      lds_steps<16, TS>(m0, tl, m[0]);
-      lds_steps<16, TS>(m1, tl, m[1]);
+    if (grow) {  // (one state at a time: no more registers than below)
+      for (int s = 0; s < S; ++s) {
+        float m[TS], H = 0.f;
+        const float A2 = as[row * Se + s];
+        lds_steps<16, TS>(cur + s * kSteps, tl, m);
 #pragma unroll
-      for (int j = 0; j < TS; ++j)
+        for (int j = 0; j < TS; ++j) H += times_exp2(v[j] * m[j], dt[j] * A2);
+        H = row_sum(H);
+        if (tl == 15) hs[row * Se + s] += H;
+      }
+    } else {
+      for (int s = 0; s < S; s += 2) {
+        const float *m0 = cur + s * kSteps, *m1 = s + 1 < S ? m0 + kSteps : zeros;
+        float m[2][TS], H[2] = {0.f, 0.f};
+        const float A2[2] = {as[row * Se + s], as[row * Se + s + 1]};
+        lds_steps<16, TS>(m0, tl, m[0]);
+        lds_steps<16, TS>(m1, tl, m[1]);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) H[i] = __builtin_fmaf(exp2_fast(dt[j] * A2[i]), v[j] * m[i][j], H[i]);
-      H[0] = row_sum(H[0]), H[1] = row_sum(H[1]);
-      if (tl == 15) hs[row * Se + s] += H[0], hs[row * Se + s + 1] += H[1];
+        for (int j = 0; j < TS; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) H[i] = __builtin_fmaf(exp2_fast(dt[j] * A2[i]), v[j] * m[i][j], H[i]);
+        H[0] = row_sum(H[0]), H[1] = row_sum(H[1]);
+        if (tl == 15) hs[row * Se + s] += H[0], hs[row * Se + s + 1] += H[1];
+      }
     }
     if (k + 1 < passes) st.store(bc + ((k + 1) & 1) * S * kSteps, S);
     __syncthreads();

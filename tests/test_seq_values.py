@@ -46,3 +46,60 @@ def test_infinite_step(N, D, L, S):
     for name, got, r, m in zip(NAMES, g, rg, mg):
         many = D if name in ("dB", "dC") else N * L / 16 if name in ("dA", "dD", "ddelta_bias") else 0
         check_finite(name, got, r, scan_tolerance(L, S) + many, m)
+
+
+GROWING = [(2, 2100, 300, 3), (1, 2100, 700, 3), (1, 6, 500, 4), (1, 6, 1500, 4), (1, 1024, 4096, 2), (1, 512, 2304, 33)]
+
+
+def growing_inputs(G, N, D, L, S):
+    """Channels of A = 1 and -1 in turn, steps of 0.5 to 0.55: e^70 over 128 steps,
+    past fp32 over 256."""
+    v = scan_inputs(G, N, D, L, S, 1, F32, False, False, False, False)
+    v["A"] = torch.ones_like(v["A"])
+    v["A"][::2] = -1
+    v["delta"] = 0.5 + 0.05 * G.u(N, D, L)
+    return v
+
+
+@pytest.mark.parametrize("N,D,L,S", GROWING)
+def test_zeros_under_growing_decays(N, D, L, S):
+    """Where a state and its gradient are zero they stay so, however far apart the
+    inputs are that decays are composed over: u begins 100 steps before the end,
+    dout ends 100 steps after the beginning."""
+    say("[gpu] zeros under growing decays", N, D, L, S)
+    G = Gen(32)
+    v = growing_inputs(G, N, D, L, S)
+    v["u"][..., :L - 100] = 0
+    do = G.n(N, D, L)
+    do[..., 100:] = 0
+    pos = [v[k] for k in ("u", "delta", "A", "B", "C")]
+    out, fin, chk = seq.selective_scan_fwd(*pos, return_final_state=True, return_checkpoints=True)
+    ref, rfin, _, _, bound, fbound = O.selective_scan(*pos)
+    check("out", out, ref, 1.0, bound)
+    check("final_state", fin, rfin, 1.0, fbound)
+    g = seq.selective_scan_bwd(do, *pos, chk)
+    rg, mg = O.selective_scan_grads(do, *pos), O.selective_scan_grads(do, *pos, absolute=True)
+    for name, got, r, m in zip(NAMES, g, rg, mg):
+        if got is not None:
+            many = D if name in ("dB", "dC") else N * L / 16 if name == "dA" else 0
+            check(name, got, r, scan_tolerance(L, S) + many, m)
+
+
+@pytest.mark.parametrize("N,D,L,S", GROWING)
+def test_small_values_grow(N, D, L, S):
+    """A value of 2e-36 grows over 250 steps to 1e18 and more, by a factor that
+    fp32 does not hold; the other steps have no length."""
+    say("[gpu] small values grow", N, D, L, S)
+    G = Gen(33)
+    v = growing_inputs(G, N, D, L, S)
+    first = L // 512 * 256
+    v["delta"][..., :first] = 0
+    v["delta"][..., first + 250:] = 0
+    v["u"].zero_()
+    v["u"][..., first] = 2e-36
+    pos = [v[k] for k in ("u", "delta", "A", "B", "C")]
+    out, fin = seq.selective_scan_fwd(*pos, return_final_state=True)
+    ref, rfin, _, _, bound, fbound = O.selective_scan(*pos)
+    assert (rfin.abs() > 1e18).any()
+    check("out", out, ref, 1.0, bound)
+    check("final_state", fin, rfin, 1.0, fbound)
