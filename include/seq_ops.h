@@ -120,7 +120,7 @@ typedef struct {
   int64_t u_n, u_d, delta_n, delta_d, z_n, z_d, dout_n, dout_d;
   int64_t B_n, B_g, B_s, C_n, C_g, C_s;
   const void *u, *delta, *z; /* [N, D, L]; z may be null                  */
-  const float* A;            /* [D, S]                                    */
+  const float* A;            /* [D, S]; -infinity: no memory, but over dt = 0 */
   const void *B, *C;         /* [N, G, S, L]                              */
   const float* Dskip;        /* [D] or null                               */
   const float* delta_bias;   /* [D] or null                               */

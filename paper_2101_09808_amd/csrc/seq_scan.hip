@@ -184,6 +184,13 @@ __device__ __forceinline__ float through(const ScanArgs<T>& a, int n, int from, 
   return h;
 }
 
+// A as the exponent of 2.  Minus infinity (a state without memory) becomes the
+// lowest finite number, so that a step of length zero leaves the state as it is.
+__device__ __forceinline__ float decay2(float A) {
+  const float A2 = kLog2e * A;
+  return A2 < -__FLT_MAX__ ? -__FLT_MAX__ : A2;  // (NaN: kept)
+}
+
 // dt of a lane's steps and its sum.  `full`: no step of the workgroup's is
 // behind the end; else those have dt = 0 (the state stands still).
 template <typename T, int TS>
@@ -235,7 +242,7 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
     float A2 = 0.f, h = 0.f;
     if (r < held) {
       const int64_t at = state_at(a, p, 0) + int64_t(r) * S + s;
-      A2 = kLog2e * a.A[s < S ? at : at - 1];
+      A2 = decay2(a.A[s < S ? at : at - 1]);
       if (s < S && a.initial) h = a.initial[int64_t(p.n) * a.D * S + at];
       if (s < S && p.seg) h = through(a, p.n, 0, p.seg * a.fine, 1, at, p.d0 + r, A2, h);
     }
@@ -400,7 +407,7 @@ __global__ __launch_bounds__(512) void scan_ends_kernel(const ScanArgs<T> a) {
   bool grow = false;  // (the wave's)
   for (int e = lane; e < 4 * Se; e += 64) {
     const int r = e / Se, s = e - r * Se;
-    const float A2 = r < p.held && s < S ? kLog2e * a.A[state_at(a, p, 0) + int64_t(r) * S + s] : 0.f;
+    const float A2 = r < p.held && s < S ? decay2(a.A[state_at(a, p, 0) + int64_t(r) * S + s]) : 0.f;
     as[e] = A2;
     hs[e] = 0.f;
     grow |= A2 > 0.f;
@@ -575,7 +582,7 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
     float A2 = 0.f, r = 0.f;
     if (r0 < held) {
       const int64_t at = state_at(a, p, 0) + int64_t(r0) * S + s;
-      A2 = kLog2e * a.A[s < S ? at : at - 1];
+      A2 = decay2(a.A[s < S ? at : at - 1]);
       if (s < S && a.dfinal) r = a.dfinal[int64_t(p.n) * a.D * S + at];
       if (s < S && p.seg < a.segs - 1)
         r = through(a, p.n, a.segs * a.fine - 1, (p.seg + 1) * a.fine - 1, -1, at, p.d0 + r0, A2, r);
@@ -923,7 +930,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
   for (int c = 0; c < CH; ++c) {
     if (c < have) load4<false>(a.A + int64_t(d0 + c * W) * a.S + s0, m, A2[c]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) A2[c][j] *= kLog2e;
+    for (int j = 0; j < 4; ++j) A2[c][j] = decay2(A2[c][j]);
   }
   const float bias = a.bias ? a.bias[d] : 0.f, skip = a.Dskip ? a.Dskip[d] : 0.f;
   struct Token {

@@ -5,7 +5,7 @@ import torch
 
 from oracle import seq as O
 from paper_2101_09808_amd import seq
-from tests.test_seq_ops import F32, Gen, check, say, scan_inputs, scan_tolerance
+from tests.test_seq_ops import DEV, F32, Gen, check, say, scan_inputs, scan_tolerance
 
 pytestmark = pytest.mark.gpu
 
@@ -103,3 +103,30 @@ def test_small_values_grow(N, D, L, S):
     assert (rfin.abs() > 1e18).any()
     check("out", out, ref, 1.0, bound)
     check("final_state", fin, rfin, 1.0, fbound)
+
+
+@pytest.mark.parametrize("N,D,L,S", [(3, 9, 150, 4), (3, 9, 700, 3), (3, 5, 2600, 16)])
+def test_states_without_memory(N, D, L, S):
+    """A = -inf: nothing of a state outlives a step, and steps behind a sequence's
+    end leave it alone.  The same bits as from a decay that underflows in each step."""
+    say("[gpu] states without memory", N, D, L, S)
+    G = Gen(34)
+    v = scan_inputs(G, N, D, L, S, 1, F32, True, True, True, True)
+    do, df = G.n(N, D, L), G.n(N, D, S)
+    lengths = torch.tensor([L, L // 2, 0], dtype=torch.int32, device=DEV)
+    kw = dict(D=v["D"], z=v["z"], delta_bias=v["delta_bias"], delta_softplus=True, lengths=lengths)
+
+    def run(a):
+        v["A"][::2, 0] = a
+        pos = [v[k] for k in ("u", "delta", "A", "B", "C")]
+        o, f, c = seq.selective_scan_fwd(*pos, initial_state=v["initial_state"], return_final_state=True,
+                                         return_checkpoints=True, **kw)
+        one = [t[..., 0] if t.dim() > 2 else t for t in pos]
+        st = v["initial_state"].clone()
+        step = seq.selective_scan_step(one[0], st, *one[1:], delta_softplus=True)
+        return [o, f, *seq.selective_scan_bwd(do, *pos, c, dfinal_state=df, **kw), step, st]
+
+    far, inf = run(-1e7), run(float("-inf"))
+    assert torch.equal(far[1][2], v["initial_state"][2])
+    for a, b in zip(far, inf):
+        assert torch.isfinite(b).all() and torch.equal(a, b)
