@@ -71,24 +71,56 @@ const Tensor& lead(PyObject* o, const char* name, int64_t rank) {
   return t;
 }
 
+// Whether a tensor has a byte in [lo, hi): its whole span first, then, if that
+// meets it, slice by slice, since a slice of a larger tensor spans what is not its own.
+bool meets(const char* p, const Tensor& t, int64_t dim, const char* lo, const char* hi) {
+  const int64_t es = int64_t(t.element_size());
+  int64_t span = 1, numel = 1;
+  for (int64_t k = dim; k < t.dim(); ++k) span += (t.size(k) - 1) * t.stride(k), numel *= t.size(k);
+  if (p >= hi || p + span * es <= lo) return false;
+  if (numel >= span) return true;
+  for (int64_t i = 0; i < t.size(dim); ++i)
+    if (meets(p + i * t.stride(dim) * es, t, dim + 1, lo, hi)) return true;
+  return false;
+}
+bool meets(const Tensor& t, const Tensor& dense) {
+  if (t.numel() == 0 || dense.numel() == 0) return false;
+  const char* lo = static_cast<const char*>(dense.data_ptr());
+  return meets(static_cast<const char*>(t.data_ptr()), t, 0, lo, lo + dense.nbytes());
+}
+
 struct Call {
+  struct Given {
+    const Tensor* t;
+    const char* name;
+  };
+  mutable Given given[16];  // the inputs (no call has more)
+  mutable int inputs = 0;
   const Tensor& like;
   c10::OptionalDeviceGuard guard;
   at::AutoDispatchBelowADInplaceOrView below;  // (results are plain tensors)
   void* stream;
 
-  explicit Call(const Tensor& t)
-      : like(t), guard(t.device()), stream(c10::hip::getCurrentHIPStream(t.device().index()).stream()) {}
+  Call(const Tensor& t, const char* name)
+      : like(t), guard(t.device()), stream(c10::hip::getCurrentHIPStream(t.device().index()).stream()) {
+    given[inputs++] = {&t, name};
+  }
 
   ScalarType type() const { return like.scalar_type(); }
 
-  const Tensor& check(PyObject* o, const char* name, IntArrayRef sizes, ScalarType t) const {
+  const Tensor& fits(PyObject* o, const char* name, IntArrayRef sizes, ScalarType t) const {
     const Tensor& x = tensor(o, name);
     if (x.scalar_type() != t)
       type_error(std::string(name) + " must be " + type_name(t) + ", got " + type_name(x.scalar_type()));
     if (x.sizes() != sizes) value_error(std::string(name) + " must be " + text(sizes) + ", got " + text(x.sizes()));
     if (x.device() != like.device())
       value_error(std::string(name) + " must be on " + like.device().str() + ", is on " + x.device().str());
+    return x;
+  }
+  const Tensor& check(PyObject* o, const char* name, IntArrayRef sizes, ScalarType t) const {
+    const Tensor& x = fits(o, name, sizes, t);
+    TORCH_INTERNAL_ASSERT(inputs < 16);
+    given[inputs++] = {&x, name};
     return x;
   }
   // The length innermost, of stride 1.
@@ -112,8 +144,34 @@ struct Call {
     // results)
     return at::cuda::empty(sizes, at::TensorOptions().dtype(t).device(like.device()));
   }
+  // A caller's tensor that the call writes, after all inputs have been checked: it
+  // may share memory with none of them (`same`: but be that one).
+  const Tensor& written(PyObject* o, const char* name, IntArrayRef sizes, ScalarType t,
+                        const Tensor* same = nullptr) const {
+    const Tensor& x = fits(o, name, sizes, t);
+    if (!x.is_contiguous()) value_error(std::string(name) + " must be contiguous");
+    apart(x, name, same);
+    return x;
+  }
+  void apart(const Tensor& x, const char* name, const Tensor* same) const {
+    for (int i = 0; i < inputs; ++i) {
+      const Tensor& in = *given[i].t;
+      if (same && &in == same && in.data_ptr() == x.data_ptr()) continue;
+      if (meets(in, x)) value_error(std::string(name) + " overlaps " + given[i].name);
+    }
+  }
   Tensor out(PyObject* o, IntArrayRef sizes, ScalarType t) const {
-    return o == Py_None ? empty(sizes, t) : dense(o, "out", sizes, t);
+    return o == Py_None ? empty(sizes, t) : written(o, "out", sizes, t);
+  }
+  // The state after a token: `o`, or in the place of `state`; `out` is apart from it.
+  void* new_state(PyObject* o, const Tensor& state, const Tensor& out) const {
+    const Tensor* to = &state;
+    if (o == Py_None)
+      apart(state, "state", &state);
+    else
+      to = &written(o, "new_state", state.sizes(), state.scalar_type(), &state);
+    if (meets(out, *to)) value_error(std::string("out overlaps ") + (o == Py_None ? "state" : "new_state"));
+    return to->data_ptr();
   }
 
   template <typename P>
@@ -189,7 +247,7 @@ seq_conv_t conv_args(const Call& c, const Tensor& x, PyObject* weight, PyObject*
 // x, weight, bias, activation, initial_state, lengths, return_final_state, out
 PyObject* conv_fwd(PyObject* const* a) {
   const Tensor& x = lead(a[0], "x", 3);
-  const Call c(x);
+  const Call c(x, "x");
   c.seq(a[0], "x", x.sizes(), c.type());
   seq_conv_t p = conv_args(c, x, a[1], a[2], a[3], a[4], a[5], "initial_state");
   const Tensor out = c.out(a[7], x.sizes(), c.type());
@@ -207,7 +265,7 @@ PyObject* conv_fwd(PyObject* const* a) {
 // dout, x, weight, bias, activation, initial_state, lengths, dfinal_state
 PyObject* conv_bwd(PyObject* const* a) {
   const Tensor& x = lead(a[1], "x", 3);
-  const Call c(x);
+  const Call c(x, "x");
   c.seq(a[1], "x", x.sizes(), c.type());
   seq_conv_t p = conv_args(c, x, a[2], a[3], a[4], a[5], a[6], "initial_state");
   const Tensor& dout = c.seq(a[0], "dout", x.sizes(), c.type());
@@ -225,13 +283,12 @@ PyObject* conv_bwd(PyObject* const* a) {
 // x, state, weight, bias, activation, new_state, out
 PyObject* conv_step(PyObject* const* a) {
   const Tensor& x = lead(a[0], "x", 2);
-  const Call c(x);
+  const Call c(x, "x");
   tensor(a[1], "state");
   seq_conv_t p = conv_args(c, x, a[2], a[3], a[4], a[1], Py_None, "state");
-  p.final_state = a[5] == Py_None ? const_cast<void*>(p.initial_state)
-                                  : c.opt<void>(a[5], "new_state", {p.N, p.D, p.R - 1}, c.type());
   const Tensor out = c.out(a[6], x.sizes(), c.type());
   p.out = out.data_ptr();
+  p.final_state = c.new_state(a[5], tensor(a[1], "state"), out);
   c.run("causal_conv_step", seq_causal_conv_step, p);
   return wrap(out);
 }
@@ -283,7 +340,7 @@ int64_t chunks_of(const seq_scan_t& p) { return (int64_t(p.L) + SEQ_SCAN_CHUNK -
 // return_final_state, return_checkpoints, out
 PyObject* scan_fwd(PyObject* const* a) {
   const Tensor& u = lead(a[0], "u", 3);
-  const Call c(u);
+  const Call c(u, "u");
   c.seq(a[0], "u", u.sizes(), c.type());
   seq_scan_t p = scan_args(c, u, a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[10]);
   p.initial_state = c.opt(a[9], "initial_state", {p.N, p.D, p.S});
@@ -303,7 +360,7 @@ PyObject* scan_fwd(PyObject* const* a) {
 // lengths, dfinal_state
 PyObject* scan_bwd(PyObject* const* a) {
   const Tensor& u = lead(a[1], "u", 3);
-  const Call c(u);
+  const Call c(u, "u");
   c.seq(a[1], "u", u.sizes(), c.type());
   seq_scan_t p = scan_args(c, u, a[2], a[3], a[4], a[5], a[7], a[8], a[9], a[10], a[11]);
   const Tensor& dout = c.seq(a[0], "dout", u.sizes(), c.type());
@@ -328,13 +385,13 @@ PyObject* scan_bwd(PyObject* const* a) {
 // u, state, delta, A, B, C, D, z, delta_bias, delta_softplus, new_state, out
 PyObject* scan_step(PyObject* const* a) {
   const Tensor& u = lead(a[0], "u", 2);
-  const Call c(u);
+  const Call c(u, "u");
   seq_scan_t p = scan_args(c, u, a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], Py_None);
-  float* const state = static_cast<float*>(c.dense(a[1], "state", {p.N, p.D, p.S}, at::kFloat).data_ptr());
-  p.initial_state = state;
-  p.final_state = a[10] == Py_None ? state : c.opt<float>(a[10], "new_state", {p.N, p.D, p.S});
+  const Tensor& state = c.dense(a[1], "state", {p.N, p.D, p.S}, at::kFloat);
+  p.initial_state = static_cast<const float*>(state.data_ptr());
   const Tensor out = c.out(a[11], u.sizes(), c.type());
   p.out = out.data_ptr();
+  p.final_state = static_cast<float*>(c.new_state(a[10], state, out));
   c.run("selective_scan_step", seq_selective_scan_step, p);
   return wrap(out);
 }
@@ -369,7 +426,7 @@ const void* strided(const Call& c, PyObject* o, const char* name, ScalarType t, 
 // x, weight, residual, scale, eps, out
 PyObject* norm_pre_fwd(PyObject* const* a) {
   const Tensor& x = lead(a[0], "x", 3);
-  const Call c(x);
+  const Call c(x, "x");
   const ScalarType rt = a[2] == Py_None ? c.type() : tensor(a[2], "residual").scalar_type();
   seq_norm_t p = norm_args(c, a[1], a[3], a[4], rt);
   p.x = strided(c, a[0], "x", c.type(), &p.x_n, &p.x_d);
@@ -383,7 +440,7 @@ PyObject* norm_pre_fwd(PyObject* const* a) {
 // dout, sum, weight, dsum, x, scale, eps
 PyObject* norm_pre_bwd(PyObject* const* a) {
   const Tensor& dout = lead(a[0], "dout", 3);
-  const Call c(dout);
+  const Call c(dout, "dout");
   const ScalarType rt = tensor(a[1], "sum").scalar_type();
   seq_norm_t p = norm_args(c, a[2], a[5], a[6], rt);
   p.dout = strided(c, a[0], "dout", c.type(), &p.dout_n, &p.dout_d);
@@ -404,7 +461,7 @@ PyObject* norm_pre_bwd(PyObject* const* a) {
 // x, weight, gate, residual, scale, eps, out
 PyObject* norm_post_fwd(PyObject* const* a) {
   const Tensor& x = lead(a[0], "x", 3);
-  const Call c(x);
+  const Call c(x, "x");
   const ScalarType rt = a[3] == Py_None ? c.type() : tensor(a[3], "residual").scalar_type();
   seq_norm_t p = norm_args(c, a[1], a[4], a[5], rt);
   p.x = strided(c, a[0], "x", c.type(), &p.x_n, &p.x_d);
@@ -419,7 +476,7 @@ PyObject* norm_post_fwd(PyObject* const* a) {
 // dout, x, weight, gate, scale, eps
 PyObject* norm_post_bwd(PyObject* const* a) {
   const Tensor& x = lead(a[1], "x", 3);
-  const Call c(x);
+  const Call c(x, "x");
   const ScalarType rt = tensor(a[0], "dout").scalar_type();
   seq_norm_t p = norm_args(c, a[2], a[4], a[5], rt);
   p.x = strided(c, a[1], "x", c.type(), &p.x_n, &p.x_d);

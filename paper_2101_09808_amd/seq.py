@@ -15,7 +15,11 @@ contiguous; parameters, scan states and ``lengths`` are fp32, fp32 and int32.
 ``lengths`` holds each sequence's valid steps, clamped to ``0..L``; what lies
 behind them is not read, and outputs and gradients are zero there.
 
-Results, and the scratch that a call needs, come from torch's allocator, so
+``out`` (of the result's size and type) takes a result in the caller's memory;
+it and ``new_state`` are contiguous and share no memory with one another or an
+input of the call, but ``new_state`` may be ``state``.
+
+Other results, and the scratch that a call needs, come from torch's allocator, so
 calls may be captured into graphs and run on any stream.  ``stream`` (a
 ``torch.cuda.Stream``; default: the current one of the tensors' device) is the
 stream that the call's kernels run on and its results belong to; ordering the
