@@ -32,6 +32,8 @@
  * their workspaces do not.  Outputs must overlap no input of the call, except
  * where stated.  The calling thread's current device must own the stream.
  *
+ * Extents: N D < 2^31, L <= 2^30; the scan's and the norms' D <= 2^30.
+ *
  * Asynchrony, errors and thread safety are those of conv_fwd.h: the calls
  * enqueue kernels on `stream` and return; CONV_EINVAL (an extent, option or
  * combination), CONV_ENULL (a required pointer), CONV_ERANGE (more work than

@@ -6,6 +6,7 @@ namespace {
 using namespace seqops;
 
 constexpr int32_t kMaxLen = 1 << 30;  // (a step index plus a tile stays in 32 bits)
+constexpr int32_t kMaxDim = 1 << 30;  // (and a channel plus a workgroup's: scan and norms)
 
 bool bad_dtype(int32_t t) { return t != CONV_DTYPE_F32 && t != CONV_DTYPE_BF16; }
 
@@ -29,14 +30,15 @@ int check_scan(const seq_scan_t* p) {
   if (const int rc = check_extents(p->N, p->D, p->L)) return rc;
   if (p->S < 1 || p->S > SEQ_SCAN_MAX_STATE || p->G < 1 || p->D % p->G || bad_dtype(p->dtype) || p->reserved)
     return CONV_EINVAL;
-  return CONV_OK;
+  return p->D > kMaxDim ? CONV_ERANGE : CONV_OK;
 }
 
 int check_norm(const seq_norm_t* p) {
   if (!p) return CONV_ENULL;
   if (const int rc = check_extents(p->N, p->D, p->L)) return rc;
   if (bad_dtype(p->dtype) || (p->res_dtype != p->dtype && p->res_dtype != CONV_DTYPE_F32)) return CONV_EINVAL;
-  return p->eps >= 0.f ? CONV_OK : CONV_EINVAL;
+  if (!(p->eps >= 0.f)) return CONV_EINVAL;
+  return p->D > kMaxDim ? CONV_ERANGE : CONV_OK;
 }
 
 bool scan_inputs(const seq_scan_t* p) { return p->u && p->delta && p->A && p->B && p->C; }
