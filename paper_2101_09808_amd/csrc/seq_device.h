@@ -168,6 +168,13 @@ __device__ __forceinline__ float softplus(float x) {
 // Keeps what follows in a branch of its own.
 __device__ __forceinline__ void branch() { asm volatile(""); }
 
+// Before lanes read what other lanes of their wave have put into LDS.  (The LDS
+// serves a wave in order: this holds the compiler to it and is no instruction.)
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // DPP moves within a row of 16 lanes or the wave.  `old` is what lanes without
 // a source keep.
 enum { kRowShl = 0x100, kRowShr = 0x110, kWaveShl1 = 0x130 };

@@ -340,6 +340,7 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
       }
     }
     if (kPer > 1 && a.checkpoints) {
+      wave_sync();
       for (int k = 1; k < kPer && t0 + k * kChunk < end; ++k)
         put(a.checkpoints + state_at(a, p, int64_t(p.n) * a.chunks + t0 / kChunk + k), mid + (k - 1) * RW * Se);
     }
@@ -788,6 +789,7 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(const ScanArgs<T> a) {
     __syncthreads();
     sum_batch(last, c0);
   }
+  wave_sync();  // (nothing to sum: dAs and rs as they were cleared)
   const int64_t at = int64_t(p.n) * a.segs + p.seg;
   const auto put = [&](float* to, const float* from) {
     for (int e = lane; e < held * S; e += 64) to[e] = from[e + e / S * (Se - S)];
