@@ -1,7 +1,9 @@
 """Build the HIP library ``libconvfwd.so`` in-tree for gfx950 with hipcc, and
-the Python module ``_seq.so`` on it.
+the Python module ``_seq.so`` (the sequence operators' calls) on it with g++ and
+torch's and Python's headers.
 
     python -m paper_2101_09808_amd.build
+    python -m paper_2101_09808_amd.build --library    # libconvfwd.so alone
 """
 import os
 import subprocess
@@ -55,15 +57,19 @@ def _build_python(verbose):
            "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "seq_python.cpp"), "-o", tmp,
            "-L", PKG, "-lconvfwd", "-L", os.path.join(torch_dir, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip",
            "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
+    try:
+        r = subprocess.run(cmd, capture_output=True, text=True)
+    except OSError as e:
+        raise RuntimeError(f"{LIB} is built, the Python module is not: {e}") from e
     if r.returncode != 0:
-        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}{r.stderr}")
+        raise RuntimeError(f"{LIB} is built, the Python module is not: {' '.join(cmd)}\n{r.stdout}{r.stderr}")
     if verbose and (r.stdout or r.stderr):
         print(r.stdout + r.stderr)
     os.replace(tmp, SEQ)
 
 
-def build(verbose=False):
+def build_library(verbose=False):
+    """libconvfwd.so, which needs hipcc and nothing else."""
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
         results = list(ex.map(_compile, SOURCES))
@@ -78,9 +84,14 @@ def build(verbose=False):
     if r.returncode != 0:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}{r.stderr}")
     os.replace(tmp, LIB)
+    return LIB
+
+
+def build(verbose=False):
+    build_library(verbose)
     _build_python(verbose)
     return LIB
 
 
 if __name__ == "__main__":
-    print(build(verbose="-v" in sys.argv))
+    print((build_library if "--library" in sys.argv else build)(verbose="-v" in sys.argv))
