@@ -21,6 +21,7 @@
 
 #include "seq_device.h"
 #include "seq_internal.h"
+#include "seq_shape.h"
 
 namespace seqops {
 namespace {
@@ -448,9 +449,8 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(const NormArgs a) {
   }
 }
 
-// Short lengths (L < 16): a sequence's [D, L] block as one run of elements.  A
-// thread keeps its column: the threads in use are a multiple of L.
-constexpr int kFlatMax = 15;
+// Short lengths (up to kFlatMax): a sequence's [D, L] block as one run of
+// elements.  A thread keeps its column: the threads in use are a multiple of L.
 
 // PHASE: as for the tiles; `stats` has [parts][NS][L] of the sequence.
 template <int PHASE, int NT, int NS>
@@ -618,68 +618,15 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* partial, in
   }
 }
 
-struct Shape {
-  bool flat;
-  int nt, cl;
-  int64_t tiles, row_tiles;  // (flat: sequences)
-  int parts, part;           // 0: the channels are not cut
-  int wgs;                   // backward: with a part of the parameters' gradients each
-};
-// Channels of a thread that stay in registers (bytes of up to four tensors' eight columns).
-int held(const seq_norm_t& p) { return p.res_dtype == CONV_DTYPE_BF16 ? 4 : 2; }
-Shape shape_of(const seq_norm_t& p) {
-  Shape s = {};
-  s.flat = p.L <= kFlatMax;
-  if (s.flat) {
-    s.tiles = p.N;
-    s.nt = int64_t(p.D) * p.L > 2048 ? 1024 : 256;
-    s.part = 256 / p.L * 8;
-  } else {
-    const auto tile = [&](int cl) {
-      s.cl = cl;
-      s.row_tiles = ceil_div(p.L, cl * 8);
-      s.tiles = s.row_tiles * p.N;
-      s.part = 256 / cl * held(p);
-    };
-    // Whole channels at once where each CU has a tile of at least 32 columns
-    // (whole cache lines of bf16) and half of its channels stay in registers;
-    // else cut.  Forward and backward, whole (at CL 2 or 4) and cut (at 8):
-    // bf16 4 x 2048 x 2048 98 and 105 us, fp32 3 x 1000 x 1333 66 and 59,
-    // bf16 9 x 2816 x 53 110 and 45.
-    tile(p.L > 32 ? 8 : p.L > 16 ? 4 : 2);
-    const auto whole = [&] { return s.tiles >= 256 && int64_t(p.D) * s.cl <= 8192; };
-    if (!whole() && s.cl == 8) {
-      tile(4);
-      if (!whole()) tile(8);
-    }
-    s.nt = int64_t(p.D) * s.cl > 512 ? 1024 : 256;
-    if (whole()) {
-      s.wgs = 256;
-      return s;
-    }
-  }
-  if (p.D >= 2 * s.part && (!s.flat || s.tiles < 128)) {
-    s.nt = 256;
-    s.parts = int(ceil_div(p.D, s.part));
-  } else {
-    while (s.cl > 2 && s.tiles < 256) {
-      s.cl /= 2;
-      s.row_tiles = ceil_div(p.L, s.cl * 8);
-      s.tiles = s.row_tiles * p.N;
-    }
-  }
-  s.wgs = int(s.parts ? s.tiles : s.flat ? (s.tiles < 512 ? s.tiles : 512) : s.tiles < 256 ? s.tiles : 256);
-  return s;
-}
-int64_t stats_floats(const seq_norm_t& p, const Shape& s, int sums) {
+int64_t stats_floats(const seq_norm_t& p, const NormShape& s, int sums) {
   return s.parts ? s.tiles * s.parts * (s.flat ? p.L : s.cl * 8) * sums : 0;
 }
-int64_t partial_floats(const seq_norm_t& p, const Shape& s) {
+int64_t partial_floats(const seq_norm_t& p, const NormShape& s) {
   return (int64_t(s.wgs) * (s.flat ? p.L : 1) * 2 * p.D + 3) / 4 * 4;
 }
 
 template <typename T, typename R, bool POST, int PHASE, int NT, int CL>
-void launch_cl(const NormArgs& a, const Shape& sh, bool bwd, hipStream_t s) {
+void launch_cl(const NormArgs& a, const NormShape& sh, bool bwd, hipStream_t s) {
   constexpr int H = sizeof(R) == 2 ? 4 : 2;
   const uint32_t wgs = uint32_t(PHASE ? sh.tiles * sh.parts : bwd ? sh.wgs : sh.tiles);
   if (bwd)
@@ -688,7 +635,7 @@ void launch_cl(const NormArgs& a, const Shape& sh, bool bwd, hipStream_t s) {
     norm_fwd_kernel<T, R, POST, PHASE, NT, CL, PHASE ? H : 2 * H><<<dim3(wgs), NT, 0, s>>>(a);
 }
 template <typename T, typename R, bool POST, int PHASE, int NT>
-void launch_nt(const NormArgs& a, const Shape& sh, bool bwd, hipStream_t s) {
+void launch_nt(const NormArgs& a, const NormShape& sh, bool bwd, hipStream_t s) {
   if (sh.flat) {
     const uint32_t wgs = uint32_t(PHASE ? sh.tiles * sh.parts : bwd ? sh.wgs : sh.tiles);
     if (bwd)
@@ -705,7 +652,7 @@ void launch_nt(const NormArgs& a, const Shape& sh, bool bwd, hipStream_t s) {
 }
 template <typename T, typename R, bool POST>
 int run(const seq_norm_t& p, bool bwd, hipStream_t s) {
-  const Shape sh = shape_of(p);
+  const NormShape sh = norm_shape(p);
   if (sh.tiles * (sh.parts ? sh.parts : 1) * sh.nt > kMaxThreads) return CONV_ERANGE;
   NormArgs a = {};
   a.N = p.N, a.D = p.D, a.L = p.L, a.eps = p.eps, a.inv_d = 1.f / float(p.D);
@@ -746,10 +693,10 @@ int run_types(const seq_norm_t& p, bool bwd, hipStream_t s) {
 }  // namespace
 
 int64_t norm_fwd_workspace(const seq_norm_t& p) {
-  return stats_floats(p, shape_of(p), 1) * int64_t(sizeof(float));
+  return stats_floats(p, norm_shape(p), 1) * int64_t(sizeof(float));
 }
 int64_t norm_bwd_workspace(const seq_norm_t& p) {
-  const Shape sh = shape_of(p);
+  const NormShape sh = norm_shape(p);
   return (partial_floats(p, sh) + stats_floats(p, sh, 2)) * int64_t(sizeof(float));
 }
 int launch_norm_fwd(const seq_norm_t& p, bool post, void* stream) {

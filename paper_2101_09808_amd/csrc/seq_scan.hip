@@ -25,11 +25,10 @@
 
 #include "seq_device.h"
 #include "seq_internal.h"
+#include "seq_shape.h"
 
 namespace seqops {
 namespace {
-
-constexpr int kChunk = SEQ_SCAN_CHUNK;  // 16 lanes of 8 steps
 
 template <typename T>
 struct ScanArgs {
@@ -995,62 +994,14 @@ __global__ __launch_bounds__(256) void scan_step_kernel(const StepArgs<T> a) {
   }
 }
 
-struct Shape {
-  int per, rows, waves, blks, segs, seg_chunks, chunks;  // rows: channels of a wave
-  int steps;  // a lane's in a pass
-  int fine, fine_chunks;
-  int64_t wgs;
-};
-Shape shape_of(const seq_scan_t& p, bool bwd) {
-  Shape s = {};
-  s.per = p.D / p.G;
-  s.chunks = int(ceil_div(p.L, kChunk));
-  const int64_t waves4 = int64_t(p.N) * p.G * ceil_div(s.per, 4);
-  s.rows = 4, s.steps = 8;
-  if (bwd) {
-    // (larger workgroups leave fewer parts of dB and dC, smaller ones start sooner:
-    // 2 x 520 x 1001 fp32, forward and backward, 52 us at eight waves, 51 at four)
-    s.waves = s.per > 16 && (waves4 > 1024 || s.chunks > 8) ? 8 : 4;
-  } else {
-    // Few and short rows: a channel has a whole wave, 512 steps a pass (which
-    // fits in LDS for up to 16 states).  2 x 520 x 1001: 15 us, against 22 in
-    // segments; 1 x 1024 x 16384: 176 us, against 145.
-    if (waves4 <= 1024 && p.L > 256 && p.L <= 2048 && p.S <= 16) s.rows = 1;
-    s.waves = p.S > 32 ? 8 : 4;
-  }
-  s.blks = int(ceil_div(s.per, s.waves * s.rows));
-  // Segments where the chip is less than half full: as many as its 2048 places
-  // for waves (two a SIMD) take at once.
-  const int64_t wgs = int64_t(p.N) * p.G * s.blks, places = 2048 / s.waves;
-  int64_t want = wgs * s.waves <= (bwd || s.rows == 1 ? 1024 : 512) ? places / wgs : 1;
-  // 16 steps a lane are a sixth less work, but a pass may waste twice as many,
-  // and two waves fit on a SIMD instead of three: for a chip that two a SIMD fill
-  // at once (4 x 2048 x 2048, forward and backward, 348 us against 355; 1 x 1024 x
-  // 16384 150 against 160), and long rows (ragged 6 x 1536 x 4000 155 against 173;
-  // ragged 12 x 4096 x 700, however, 164 against 131).
-  if (!bwd && s.rows == 4 && p.S <= 16 && ceil_div(p.L, 256) * 12 <= ceil_div(p.L, 128) * 7 && want * 256 <= p.L &&
-      (wgs * s.waves * want <= 2048 || p.L > 2048))
-    s.steps = 16;
-  const int per = 64 / s.rows * s.steps / kChunk;  // chunks a pass
-  const int64_t passes = ceil_div(s.chunks, per);
-  if (want > passes) want = passes;
-  s.seg_chunks = int(ceil_div(passes, want)) * per;
-  s.segs = int(ceil_div(s.chunks, s.seg_chunks));
-  s.wgs = wgs * s.segs;
-  // (pieces of 256 steps at least, up to 4096 waves of them)
-  s.fine = 1;
-  while (s.fine < 4 && waves4 * (s.segs - 1) * s.fine * 2 <= 4096 && s.seg_chunks >= 4 * s.fine) s.fine *= 2;
-  s.fine_chunks = int(ceil_div(s.seg_chunks, s.fine));
-  return s;
-}
 int64_t pad4(int64_t n) { return (n + 3) / 4 * 4; }
-int64_t ends_floats(const seq_scan_t& p, const Shape& s) {
+int64_t ends_floats(const seq_scan_t& p, const ScanShape& s) {
   const int64_t pieces = int64_t(p.N) * s.segs * s.fine;
   return s.segs > 1 ? pad4(pieces * p.D * p.S) + pad4(pieces * p.D) : 0;
 }
 
 template <typename T>
-ScanArgs<T> args_of(const seq_scan_t& p, const Shape& s) {
+ScanArgs<T> args_of(const seq_scan_t& p, const ScanShape& s) {
   ScanArgs<T> a = {};
   a.N = p.N, a.D = p.D, a.L = p.L, a.S = p.S, a.G = p.G, a.per = s.per, a.softplus = p.delta_softplus;
   a.blks = s.blks, a.segs = a.run_segs = s.segs, a.seg_chunks = s.seg_chunks, a.chunks = s.chunks;
@@ -1089,7 +1040,7 @@ int with_loads(int rows, int pass, int waves, F f) {
 }
 
 template <typename T, int TS, bool BACK>
-int ends_steps(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, int64_t wgs, hipStream_t st) {
+int ends_steps(const seq_scan_t& p, const ScanShape& s, const ScanArgs<T>& a, int64_t wgs, hipStream_t st) {
   const int64_t lds = ((2 * p.S + 1) * int64_t(16 * TS) + 4 * 8 * ((p.S + 1) & ~1)) * 4;
   return with_loads<4>(p.S, 16 * TS, 4, [&](auto nb) {
     return launch(scan_ends_kernel<T, TS, decltype(nb)::value, BACK>, wgs, 256, lds, st, a);
@@ -1097,7 +1048,7 @@ int ends_steps(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, int64_
 }
 // The ends of all segments but the last (BACK: the first), which nothing comes after.
 template <typename T, bool BACK>
-int ends_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st) {
+int ends_pass(const seq_scan_t& p, const ScanShape& s, ScanArgs<T> a, hipStream_t st) {
   a.blks = int(ceil_div(s.per, 16));
   a.run_segs = (s.segs - 1) * s.fine, a.run_first = BACK ? s.fine : 0;
   const int64_t wgs = int64_t(p.N) * p.G * a.blks * a.run_segs;
@@ -1106,7 +1057,7 @@ int ends_pass(const seq_scan_t& p, const Shape& s, ScanArgs<T> a, hipStream_t st
 }
 
 template <typename T, int RW, int TS>
-int fwd_pass(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
+int fwd_pass(const seq_scan_t& p, const ScanShape& s, const ScanArgs<T>& a, hipStream_t st) {
   constexpr int pass = 64 / RW * TS, per = pass / kChunk;
   const int64_t lds = ((4 * p.S + 1) * int64_t(pass) + s.waves * (1 + per) * RW * ((p.S + 1) & ~1)) * 4;
   // (512 steps of 32 rows by 4 waves; else 256 of 32 or 128 of 64 by 4, 128 of 128 by 8)
@@ -1116,7 +1067,7 @@ int fwd_pass(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStrea
 }
 template <typename T>
 int fwd(const seq_scan_t& p, hipStream_t st) {
-  const Shape s = shape_of(p, false);
+  const ScanShape s = scan_shape(p, false);
   if (s.wgs * s.waves * 64 > kMaxThreads) return CONV_ERANGE;
   if (s.segs > 1 && !p.workspace) return CONV_ENULL;
   if (s.segs > 1 && p.workspace_bytes < scan_fwd_workspace(p)) return CONV_ESCRATCH;
@@ -1131,10 +1082,8 @@ int fwd(const seq_scan_t& p, hipStream_t st) {
   return s.steps == 16 ? fwd_pass<T, 4, 16>(p, s, a, st) : fwd_pass<T, 4, 8>(p, s, a, st);
 }
 
-// As many as LDS holds beside what S states need: an exchange is two barriers.
-int batch_of(int S) { return S > 32 ? 4 : S > 16 || S <= 8 ? 8 : 16; }
 template <typename T, bool GATE>
-int bwd_pass(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStream_t st) {
+int bwd_pass(const seq_scan_t& p, const ScanShape& s, const ScanArgs<T>& a, hipStream_t st) {
   const int rows = 2 * p.S, Se = (p.S + 1) & ~1;
   const int64_t lds = ((rows + 1) * int64_t(kChunk) + a.batch * s.waves * 256 + s.waves * 16 * Se) * 4;
   return with_loads<8>(rows, kChunk, s.waves, [&](auto nb) {
@@ -1143,14 +1092,14 @@ int bwd_pass(const seq_scan_t& p, const Shape& s, const ScanArgs<T>& a, hipStrea
 }
 template <typename T>
 int bwd(const seq_scan_t& p, hipStream_t st) {
-  const Shape s = shape_of(p, true);
+  const ScanShape s = scan_shape(p, true);
   const int64_t bc_wgs = ceil_div(int64_t(p.N) * p.G * p.S * 2 * s.chunks * (kChunk / 4), 256);
   const int64_t sum_wgs = bc_wgs + ceil_div(int64_t(p.D) * (p.S + 2), 256);
   if (s.wgs * s.waves * 64 > kMaxThreads || sum_wgs * 256 > kMaxThreads) return CONV_ERANGE;
   if (!p.workspace) return CONV_ENULL;
   if (p.workspace_bytes < scan_bwd_workspace(p)) return CONV_ESCRATCH;
   ScanArgs<T> a = args_of<T>(p, s);
-  a.batch = batch_of(p.S);
+  a.batch = scan_batch(p.S);
   a.part_bc = static_cast<float*>(p.workspace);
   a.part_A = a.part_bc + int64_t(p.N) * p.G * s.blks * p.S * 2 * s.chunks * kChunk;
   a.part_D = a.part_A + pad4(int64_t(p.N) * s.segs * p.D * p.S);
@@ -1200,10 +1149,10 @@ int step(const seq_scan_t& p, hipStream_t st) {
 }  // namespace
 
 int64_t scan_fwd_workspace(const seq_scan_t& p) {
-  return ends_floats(p, shape_of(p, false)) * int64_t(sizeof(float));
+  return ends_floats(p, scan_shape(p, false)) * int64_t(sizeof(float));
 }
 int64_t scan_bwd_workspace(const seq_scan_t& p) {
-  const Shape s = shape_of(p, true);
+  const ScanShape s = scan_shape(p, true);
   const int64_t rows = int64_t(p.N) * s.segs * p.D;
   return (int64_t(p.N) * p.G * s.blks * p.S * 2 * s.chunks * kChunk + pad4(rows * p.S) + pad4(rows * 2) +
           ends_floats(p, s)) * int64_t(sizeof(float));
