@@ -196,6 +196,93 @@ def selective_scan_grads(dout, u, delta, A, B, C, D=None, z=None, delta_bias=Non
     return du * mask, ddelta, dA, dB, dC, (dy * u).sum((0, 2)), ddelta.sum((0, 2)), g * y * dgate, r
 
 
+def selective_scan_grad_bounds(dout, u, delta, A, B, C, D=None, z=None, delta_bias=None, delta_softplus=False,
+                               initial_state=None, lengths=None, dfinal_state=None, cut=None):
+    """The gradients again, and bounds (in units of 2^-24) of what fp32 arithmetic
+    may be off by in each, carried along both recurrences: (grads, bounds), in the
+    order of :func:`selective_scan_grads`.
+
+    What is counted: a gradient of a state is off by what reaches it of the next
+    step's, decayed, and its own roundings, as a state is in
+    :func:`selective_scan`; a product by each factor's error times the other one's
+    magnitude, and its rounding; a sum by its terms' errors and one rounding of the
+    whole (in absolute values) for each level of the tree it is formed by.  `cut`:
+    the segments of a sequence and their chunks of 128 steps (else one).
+    """
+    G = B.shape[1]
+    _, _, before, y, ybound, _ = selective_scan(u, delta, A, B, C, D, None, delta_bias, delta_softplus, initial_state,
+                                                lengths)
+    u, raw, dt, A, Be, Ce, z, mask = _scan_inputs(u, delta, A, B, C, z, delta_bias, delta_softplus, lengths)
+    N, Dn, L = u.shape
+    S = A.shape[1]
+    g = _clean(d(dout), mask.expand(N, Dn, L))
+    zero = torch.zeros_like(u)
+    gate, dgate, mdgate, az = torch.ones_like(u), zero, zero, zero
+    if z is not None:
+        s = torch.sigmoid(z)
+        gate, dgate, mdgate, az = silu(z), dsilu(z), s * (1 + z.abs() * (1 - s)), z.abs()
+    dy = g * gate
+    # relative, in 2^-24: dt and dy (a sigmoid: its rounded exponent and four more,
+    # two products), the slope of softplus
+    edt = (2.5 * raw.abs() + 10 if delta_softplus else torch.ones_like(raw)) * mask
+    edy = (2 * az + 8 if z is not None else zero)
+    eslope = 3 * raw.abs() + 6
+    x = dt * u
+    # the states' errors
+    h = torch.zeros((N, Dn, S), dtype=F64) if initial_state is None else d(initial_state)
+    m, herr = h.abs(), [torch.zeros_like(h)]
+    for t in range(L):
+        a, xb = torch.exp(dt[..., t, None] * A), x[..., t, None].abs() * Be[..., t].abs()
+        decay = 8 + (8 + edt[..., t, None]) * (A * dt[..., t, None]).abs()
+        m = a * m + xb
+        herr.append(a * herr[-1] + m * decay + xb * edt[..., t, None])
+    # levels of sums: a wave's four channels, a workgroup's waves, the workgroups; 8
+    # steps of a lane, 4 levels over lanes, the chunks of a segment (dD and
+    # ddelta_bias: all steps of a lane before the lanes) and then the segments and
+    # sequences one by one
+    per, (segs, chunks) = Dn // G, cut or (1, -(-L // 128))
+    over_channels, over_steps = 2 + 8 + -(-per // 16), 12 + chunks + N * segs
+    over_elements = 8 * chunks + 4 + N * segs
+    r = torch.zeros((N, Dn, S), dtype=F64) if dfinal_state is None else d(dfinal_state)
+    mr, er = r.abs(), torch.zeros_like(r)
+    dA, edA = torch.zeros_like(A), torch.zeros_like(A)
+    ddt, eddt, dx, edx = (torch.zeros_like(u) for _ in range(4))
+    dB, dC = torch.zeros_like(Be), torch.zeros_like(Ce)
+    edB, edC = torch.zeros_like(Be), torch.zeros_like(Ce)
+    for t in reversed(range(L)):
+        p, hp, ehp = dt[..., t, None], before[t], herr[t]
+        a, decay = torch.exp(p * A), 8 + (8 + edt[..., t, None]) * (A * p).abs()
+        c, b, q, xt = Ce[..., t], Be[..., t], dy[..., t, None], x[..., t, None]
+        ht, eht = a * hp + xt * b, herr[t + 1]
+        e, me = r + q * c, mr + (q * c).abs()
+        ee = er + (q * c).abs() * (edy[..., t, None] + 1) + me
+        dC[..., t], edC[..., t] = q * ht, q.abs() * eht + (q * ht).abs() * (edy[..., t, None] + 2 + over_channels)
+        dB[..., t] = e * xt
+        edB[..., t] = ee * xt.abs() + (e * xt).abs() * (edt[..., t, None] + 3 + over_channels)
+        dx[..., t], edx[..., t] = (e * b).sum(-1), ((ee + e.abs() * (S + 1)) * b.abs()).sum(-1)
+        r, mr, er = a * e, a * me, a * ee + a * me * decay
+        k = r * hp
+        ek = 1.01 * (er * hp.abs() + r.abs() * ehp) + k.abs()
+        ddt[..., t], eddt[..., t] = (k * A).sum(-1), ((ek + k.abs() * (S + 4)) * A.abs()).sum(-1)
+        dA += (k * p).sum(0)
+        edA += ((ek + k.abs() * (edt[..., t, None] + 2 + over_steps)) * p.abs()).sum(0)
+    skip = torch.zeros(Dn, dtype=F64) if D is None else d(D)
+    slope = torch.sigmoid(raw) if delta_softplus else torch.ones_like(raw)
+    ddelta = (ddt + dx * u) * slope * mask
+    eddelta = (edx * u.abs() + eddt + 3 * ((dx * u).abs() + ddt.abs())) * slope * mask
+    if delta_softplus:
+        eddelta = eddelta + ddelta.abs() * (eslope + 1)
+    sk = (skip[:, None] * dy).abs()
+    du, edu = dx * dt + skip[:, None] * dy, edx * dt.abs() + (dx * dt).abs() * (edt + 2) + sk * (edy + 2)
+    fold = lambda v: v.view(N, G, per, S, L).sum(2) * mask[:, None]  # noqa: E731
+    # (ybound is the ungated y's)
+    edz = (g * dgate).abs() * ybound + (g * y).abs() * mdgate * (4 * az + 16)
+    grads = (du * mask, ddelta, dA, fold(dB), fold(dC), (dy * u).sum((0, 2)), ddelta.sum((0, 2)), g * y * dgate, r)
+    bounds = (edu * mask, eddelta, edA, fold(edB), fold(edC), ((dy * u).abs() * (edy + 2 + over_elements)).sum((0, 2)),
+              (eddelta + ddelta.abs() * over_elements).sum((0, 2)), edz, er)
+    return grads, bounds
+
+
 # ------------------------------------------------------------------------ norms
 
 def norm_pre(x, weight, residual=None, scale=None, eps=1e-6):
