@@ -151,7 +151,8 @@ __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf
 // log(1 + exp(x)) = max(x, 0) + log1p(e), e = exp(-|x|) in (0, 1], and
 // log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3: steps of 1e-3 keep their
 // digits.  2 artanh(s) / s is a polynomial in q = s^2, interpolated at the
-// Chebyshev nodes of [0, 1/9] (within 4e-9 of it).
+// Chebyshev nodes of [0, 1/9] (with these fp32 coefficients within 1.6e-8 of it, a
+// relative 7.7e-9).
 __device__ __forceinline__ float softplus(float x) {
   const float e = exp2_fast(-kLog2e * __builtin_fabsf(x));
   const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;

@@ -19,8 +19,8 @@
 // segment alone makes of a zero state, the second composes those before its own.
 //
 // Forward, bf16, 4 x 2048 x 2048 with 16 states and gate (2^28 steps of states):
-// 80 us, 10.4 issue slots a step of a state (7 of them the recurrence itself),
-// slots in use 82% of the time.  1 x 1024 x 16384 (2^28 too, cut into 8): 145 us.
+// 89 us, 10.4 issue slots a step of a state (7 of them the recurrence itself),
+// slots in use 82% of the time.  1 x 1024 x 16384 (2^28 too, cut into 8): 146 us.
 #include <type_traits>
 
 #include "seq_device.h"

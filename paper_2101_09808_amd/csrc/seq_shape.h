@@ -21,8 +21,12 @@ inline ScanShape scan_shape(const seq_scan_t& p, bool bwd) {
   const int64_t waves4 = int64_t(p.N) * p.G * ceil_div(s.per, 4);
   s.rows = 4, s.steps = 8;
   if (bwd) {
-    // (larger workgroups leave fewer parts of dB and dC, smaller ones start sooner:
-    // 2 x 520 x 1001 fp32, forward and backward, 52 us at eight waves, 51 at four)
+    // Larger workgroups leave fewer parts of dB and dC, smaller ones spread few
+    // channels further.  Backward at four and at eight waves, us: 2 x 520 x 260 fp32,
+    // 8 states, 28.0 and 29.5; 2 x 520 x 1500 47.6 and 47.1; 1 x 64 x 1000 bf16, 16
+    // states, 29.7 and 33.9; 1 x 1024 x 2048 75 and 56; 8 x 2048 x 500 215 and 143.
+    // (With 16 states eight are faster below nine chunks, too, where the channels are
+    // not few: 2 x 520 x 1001 69 and 51.)
     s.waves = s.per > 16 && (waves4 > 1024 || s.chunks > 8) ? 8 : 4;
   } else {
     // Few and short rows: a channel has a whole wave, 512 steps a pass (which
@@ -82,11 +86,18 @@ inline NormShape norm_shape(const seq_norm_t& p) {
       s.tiles = s.row_tiles * p.N;
       s.part = 256 / cl * norm_held(p);
     };
-    // Whole channels at once where each CU has a tile of at least 32 columns
-    // (whole cache lines of bf16) and half of its channels stay in registers;
-    // else cut.  Forward and backward, whole (at CL 2 or 4) and cut (at 8):
-    // bf16 4 x 2048 x 2048 98 and 105 us, fp32 3 x 1000 x 1333 66 and 59,
-    // bf16 9 x 2816 x 53 110 and 45.
+    // Whole channels at once where each CU has a tile of at least 32 columns (half a
+    // cache line of bf16; the next tile's workgroup is of the same XCD) and at least
+    // half of its channels (fp32 residual: a quarter) stay in registers over the
+    // backward pass; else cut.  Forward and backward after a block, gated, us for
+    // N x D x 2048, whole and cut, with a bf16 residual | an fp32 one (x in bf16):
+    //   4 x 1024   44,  52 |  48,  62     16 x 1024  165, 192 |  218,  240
+    //   4 x 1536   60,  80 |  79,  95     16 x 1536  290, 301 |  363,  366
+    //   4 x 2048  100, 103 | 116, 129     16 x 2048  390, 388 |  522,  496
+    //   4 x 2560  126, 133 | 151, 163     16 x 2560  520, 488 |  623,  642
+    // The bound on D CL, 8192, lies where the two meet; over many tiles they do a
+    // little before it, over few a little behind.  Too few tiles to be whole:  fp32
+    // 3 x 1000 x 1333 66 and 59, bf16 9 x 2816 x 53 110 and 45.
     tile(p.L > 32 ? 8 : p.L > 16 ? 4 : 2);
     const auto whole = [&] { return s.tiles >= 256 && int64_t(p.D) * s.cl <= 8192; };
     if (!whole() && s.cl == 8) {
