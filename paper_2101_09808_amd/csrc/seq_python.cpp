@@ -151,7 +151,13 @@ struct Call {
     const Tensor& x = fits(o, name, sizes, t);
     if (!x.is_contiguous()) value_error(std::string(name) + " must be contiguous");
     apart(x, name, same);
+    touch(x);
     return x;
+  }
+  // What autograd has saved of it is no longer what it was: a backward pass that
+  // needs it raises.
+  static void touch(const Tensor& x) {
+    if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version();
   }
   void apart(const Tensor& x, const char* name, const Tensor* same) const {
     for (int i = 0; i < inputs; ++i) {
@@ -167,7 +173,7 @@ struct Call {
   void* new_state(PyObject* o, const Tensor& state, const Tensor& out) const {
     const Tensor* to = &state;
     if (o == Py_None)
-      apart(state, "state", &state);
+      apart(state, "state", &state), touch(state);
     else
       to = &written(o, "new_state", state.sizes(), state.scalar_type(), &state);
     if (meets(out, *to)) value_error(std::string("out overlaps ") + (o == Py_None ? "state" : "new_state"));

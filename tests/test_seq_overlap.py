@@ -69,3 +69,22 @@ def test_a_states_other_view_is_the_state():
     new = torch.empty_like(st)
     ref = seq.causal_conv_step(x, keep, w, new_state=new)
     assert torch.equal(seq.causal_conv_step(x, st, w, new_state=st.view(3, 5, 3)), ref) and torch.equal(st, new)
+
+
+def test_autograd_sees_what_is_written():
+    """A tensor that autograd saved and a call wrote over raises in the backward
+    pass, where it would give a gradient of other values."""
+    G = Gen(45)
+    x, w, st, out = G.n(3, 5), G.n(5, 4), G.n(3, 5, 3), torch.zeros(3, 5, device="cuda")
+    p = torch.ones((), device="cuda", requires_grad=True)
+    for t, f in ((st, lambda: seq.causal_conv_step(x, st, w)),
+                 (st, lambda: seq.causal_conv_step(x, G.n(3, 5, 3), w, new_state=st)),
+                 (out, lambda: seq.causal_conv_step(x, G.n(3, 5, 3), w, out=out))):
+        y = (t * p).sum()
+        f()
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.backward()
+    with torch.inference_mode():
+        s2 = st.clone()
+    seq.causal_conv_step(x, s2, w)
+    (x * p).sum().backward()  # (inputs are as they were)
