@@ -10,7 +10,7 @@ the ``_bwd`` functions.
 
 Sequences (``x``, ``u``, ``delta``, ``z``, ``B``, ``C``, ``gate``, ``residual``
 and gradients that come in) are fp32 or bf16 with the length innermost and of
-stride 1; their other strides are free.  Parameters, states and ``lengths`` are
+stride 1; their other strides are free, and no extent is zero.  Parameters, states and ``lengths`` are
 contiguous; parameters, scan states and ``lengths`` are fp32, fp32 and int32.
 ``lengths`` holds each sequence's valid steps, clamped to ``0..L``; what lies
 behind them is not read, and outputs and gradients are zero there.
