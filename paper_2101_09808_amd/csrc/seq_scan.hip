@@ -382,10 +382,10 @@ __global__ __launch_bounds__(512) void scan_fwd_kernel(const ScanArgs<T> a) {
 // by side, weighted with their decay to that end, so a state needs no scan, only
 // a sum over the row; the decays' exponents are sums of dt, taken along as the
 // passes walk away from the end.  Where those decays may grow (some A is positive, or
-// without softplus a step negative) they are past fp32 over a piece when they are
-// not over kChunk steps, and go into each product without being formed.  A segment is cut further (`fine`), for more waves
-// than the scan's registers allow: 1 x 1024 x 16384, 16 states, seven segments of
-// eight, 63 us whole and 59 in two pieces each.
+// without softplus a step negative) they can be past fp32 over a piece when they are
+// not over kChunk steps, and go into each product without being formed.  A segment is
+// cut further (`fine`), for more waves than the scan's registers allow: 1 x 1024 x
+// 16384, 16 states, seven segments of eight, 63 us whole and 59 in two pieces each.
 template <typename T, int TS, int NB, bool BACK>
 __global__ __launch_bounds__(512) void scan_ends_kernel(const ScanArgs<T> a) {
   extern __shared__ float lds[];
