@@ -14,8 +14,8 @@ def inputs(N, D, L, S, G, gate, soft, extra, seed=7):
     v = dict(u=n(N, D, L), delta=n(N, D, L) * 0.5)
     if not soft:
         v["delta"] = v["delta"].abs() * 0.1
-    v.update(A=-torch.arange(1, S + 1.) * (0.5 + torch.rand(D, 1, generator=g)), B=n(N, G, S, L), C=n(N, G, S, L),
-             D=n(D) if extra else None, z=n(N, D, L) if gate else None,
+    v.update(A=-torch.arange(1, S + 1.) * (0.5 + torch.rand(D, 1, generator=g)),
+             B=n(N, G, S, L), C=n(N, G, S, L), D=n(D) if extra else None, z=n(N, D, L) if gate else None,
              delta_bias=-4 * torch.rand(D, generator=g) - 1 if extra else None)
     return (n(N, D, L), *v.values(), soft, n(N, D, S))
 

@@ -14,7 +14,8 @@ SCAN = [
     # 16 steps a lane in segments cut into pieces; eight waves over segments of several chunks
     ((2, 320, 4200, 11, 16, BF, True, (4200, 1999)), dict(rows=4, steps=16, segs=6, seg_chunks=6, fine=2),
      dict(waves=8, segs=7, seg_chunks=5, fine=2, fine_chunks=3, batch=16)),
-    ((1, 64, 8300, 5, 64, F32, True, None), dict(steps=16, segs=7, fine=4), dict(waves=4, segs=8, seg_chunks=9, fine=4)),
+    ((1, 64, 8300, 5, 64, F32, True, None), dict(steps=16, segs=7, fine=4),
+     dict(waves=4, segs=8, seg_chunks=9, fine=4)),
     # eight waves, whole sequences of several chunks, for each batch of states
     ((65, 64, 300, 16, 1, F32, True, (300, 129, 0, 77)), dict(rows=4, steps=8, segs=1),
      dict(waves=8, segs=1, chunks=3, batch=16)),
@@ -75,7 +76,9 @@ def test_scan_instances(case):
     say("[gpu] scan instance", case[0])
     G = Gen(51)
     v = scan_inputs(G, N, D, L, S, Gr, t, gate, True, True, True)
-    lengths = None if lens is None else torch.tensor([lens[n % len(lens)] for n in range(N)], dtype=torch.int32, device=DEV)
+    lengths = None
+    if lens is not None:
+        lengths = torch.tensor([lens[n % len(lens)] for n in range(N)], dtype=torch.int32, device=DEV)
     do, df = spoil(G.n(N, D, L, dtype=t), lengths), G.n(N, D, S)
     for k in ("u", "delta", "B", "C", "z"):
         if v[k] is not None:

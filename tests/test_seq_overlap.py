@@ -40,7 +40,8 @@ def test_states_over_inputs():
     refused("state overlaps x", seq.causal_conv_step, buf[:N * D].view(N, D), st, w)
     refused("out overlaps state", seq.causal_conv_step, x, st, w, out=buf[1:1 + N * D].view(N, D))
     new = torch.empty_like(st)
-    refused("out overlaps new_state", seq.causal_conv_step, x, st, w, new_state=new, out=new.view(-1)[:N * D].view(N, D))
+    refused("out overlaps new_state", seq.causal_conv_step, x, st, w, new_state=new,
+            out=new.view(-1)[:N * D].view(N, D))
     v = scan_inputs(G, N, D, 1, S, 1, F32, False, True, False, True)
     u, delta, A, B, C = (v[k][..., 0] if v[k].dim() > 2 else v[k] for k in ("u", "delta", "A", "B", "C"))
     delta, h = delta.contiguous(), v["initial_state"]
